@@ -400,6 +400,79 @@ int is_gemm_w4a8_intscale_safe(const int8_t* xq, const float* a_scale, const voi
 size_t is_gemm_safe_workspace_bytes(int M, int N, int K, int group);
 
 /*
+ * Between a block's projections.  Queries, keys and values are fp16 rows of heads side by side, as a qkv projection writes
+ * them: head h of row m begins at base + m * ld + h * head_dim (ld in elements, a multiple of 8, at least the heads' width), so
+ * that q, k and v may be the columns of one buffer.  Device arrays of lengths and places are read by the kernels alone; what they
+ * hold is bounded there and never leads outside the tensors.
+ *
+ * Per-head RMSNorm of queries and keys and the rotation by position, in one pass:
+ *   y[i] = x[i] * gamma[i] / sqrt(mean(x^2) + eps)   over the head's head_dim columns (gamma NULL: y = x, eps ignored)
+ *   (y[a], y[b]) -> (y[a] cos t - y[b] sin t, y[b] cos t + y[a] sin t),  t = positions[m] * inv_freq[i],  i < rot_dim / 2
+ *   with (a, b) = (i, i + rot_dim / 2), or (2 i, 2 i + 1) when interleaved is 1; the columns from rot_dim on stay y.
+ * Single precision throughout (the angle in double), rounded once to fp16.
+ *   q, q_out     fp16 [M] rows of heads_q heads;  k, v fp16 [M] rows of heads_k heads (v and v_out both NULL: no values)
+ *   gamma_q, gamma_k   fp16 [head_dim], each may be NULL
+ *   inv_freq     float [rot_dim / 2] (may be NULL when rot_dim is 0);  positions  int32 [M]
+ *   kv_rows      int64 [M] or NULL.  NULL: row m of k and v goes to row m of k_out and v_out.  Otherwise to row kv_rows[m], the
+ *                token's row of a cache; a row outside [0, cache_rows) goes nowhere (a padding token's -1), and rows of the
+ *                cache that no token names stay as they are.  No two tokens may name the same row.
+ *   cache_rows   rows of k_out and v_out
+ * q_out may be q, and without kv_rows k_out may be k and v_out may be v (same ld); otherwise outputs and inputs must not overlap.
+ * Requirements: head_dim a multiple of 8, at most 256; rot_dim a multiple of 8, at most head_dim; at most 1024 heads, M at most
+ * 2^20.  heads_q or heads_k (not both) may be 0; then its pointers are not looked at.
+ */
+int is_qk_norm_rope(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* gamma_q,
+                    const void* gamma_k, float eps, const float* inv_freq, int rot_dim, int interleaved,
+                    const int32_t* positions, const int64_t* kv_rows, int M, int heads_q, int heads_k, int head_dim,
+                    int64_t cache_rows, void* q_out, int64_t ldqo, void* k_out, int64_t ldko, void* v_out, int64_t ldvo,
+                    void* stream);
+
+/*
+ * Attention over packed sequences of different lengths, grouped heads: for row i of a sequence with q_len rows and kv_len keys
+ *   out[i, h] = fp16( sum_j p[j] v[j, h / g] ),  p = softmax_j( scale * q[i, h] . k[j, h / g] ),  g = heads_q / heads_kv
+ *   over j < kv_len, and with causal = 1 over j <= i + kv_len - q_len: the last row sees every key (q_len = 1 is a decode step,
+ *   q_len = kv_len a whole prompt, anything between a chunk of one).  A row that sees no key (kv_len = 0, or kv_len < q_len and
+ *   a row before the first key) is zero.
+ * Scores, softmax statistics and sums in single precision; the probabilities are rounded to fp16 for their product with v.  What
+ * a row does not see does not reach it, whatever it holds (infinities and NaN among it).
+ *   q, out       fp16 [M] rows of heads_q heads;  k, v  fp16 [kv_rows] rows of heads_kv heads
+ *   q_offsets    int32 [num_seqs + 1], non-decreasing: rows [q_offsets[s], q_offsets[s+1]) of q and out are sequence s's.  Rows of
+ *                out that belong to no sequence stay as they are.
+ *   kv_starts    int64 [num_seqs] or NULL: the sequence's first row of k and v (NULL: q_offsets[s]).  Sequences may share rows.
+ *   kv_lens      int32 [num_seqs] or NULL: its number of keys (NULL: its number of rows of q).  A sequence whose start lies outside
+ *                [0, kv_rows] has none; one that runs over the end of k and v ends there.
+ *   max_q_len, max_kv_len   no sequence is longer (they choose the kernel and the split of the keys; keys past max_kv_len are left out)
+ *   workspace    at least is_attention_workspace_bytes(...) bytes (0 when the keys are not split), contents arbitrary
+ * Rows of out are written whole; out must not overlap the inputs.  Results do not depend on how a batch's sequences are mixed,
+ * but for the split of the keys, which depends on M, num_seqs and the maxima alone.
+ * Requirements: head_dim 64 or 128 (IS_ERR_UNSUPPORTED otherwise), heads_kv dividing heads_q, at most 1024 heads, M at most 2^20,
+ * max_kv_len at most 2^30, ldk and ldv at most 2^23, (M * g / 32 + num_seqs) * heads_kv at most 2^22; scale positive and finite.
+ */
+size_t is_attention_workspace_bytes(int M, int num_seqs, int max_q_len, int max_kv_len, int heads_q, int heads_kv, int head_dim);
+int is_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const int32_t* q_offsets,
+                 const int64_t* kv_starts, const int32_t* kv_lens, int M, int64_t kv_rows, int num_seqs, int max_q_len,
+                 int max_kv_len, int heads_q, int heads_kv, int head_dim, float scale, int causal, void* out, int64_t ldo,
+                 void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Low-rank adapters of many requests beside a shared projection: with e = row_adapter[m],
+ *   out[m,n] = fp16( base[m,n] + scales[e] * sum_r (sum_k x[m,k] a[e,r,k]) * b[e,n,r] ),  r < ranks[e];
+ *   rows whose adapter lies outside [0, num_adapters) (-1: none) get base[m,n].
+ * Sums in single precision.
+ *   x    fp16 [M] rows of K elements, ldx apart;  a  fp16 [num_adapters, R, K];  b  fp16 [num_adapters, N, R]
+ *   row_adapter  int32 [M];  scales  float [num_adapters] or NULL (1);  ranks  int32 [num_adapters] or NULL (R): what lies past an
+ *                adapter's rank (rows of a, columns of b) does not count
+ *   base, out    fp16 [M] rows of N elements, ldb and ldo apart.  base is the projection's output (NULL: zeros); out may be base
+ *                (ldo = ldb; rows without an adapter are then left alone)
+ *   workspace    at least is_lora_workspace_bytes(...) bytes, contents arbitrary
+ * Requirements: K and R multiples of 8, R at most 128, ldx a multiple of 8; M, N, K and num_adapters at most 2^20.
+ */
+size_t is_lora_workspace_bytes(int M, int N, int K, int R, int num_adapters);
+int is_lora_add(const void* x, int64_t ldx, const void* a, const void* b, const int32_t* row_adapter, const float* scales,
+                const int32_t* ranks, int M, int N, int K, int R, int num_adapters, const void* base, int64_t ldb, void* out,
+                int64_t ldo, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Measurement aids (no part of the method): the two rates the GEMMs are priced against, as this chip delivers them.
  *   is_probe_stream_read  reads `bytes` bytes (a multiple of 16) at `src` (device) once, 16 bytes per lane
  *   is_probe_mfma_i8      every wave of a chip-filling launch issues `iters` rounds of 16 independent

@@ -1,10 +1,12 @@
 // C ABI of the library: argument validation (before any HIP call) and dispatch to the gfx950 kernels.
+#include <math.h>
 #include <stdlib.h>
 #include <string.h>
 
 #include <algorithm>
 #include <mutex>
 
+#include "block_common.h"
 #include "few_common.h"
 #include "is_common.h"
 #include "pk_common.h"
@@ -968,6 +970,170 @@ int is_intscale_overflow_bound(const int32_t* scale_i32, int N, int K, int group
     if (!ok_ptr(scale_i32) || bound_dev == nullptr || (reinterpret_cast<uintptr_t>(bound_dev) & 7u))
         return IS_ERR_INVALID_ARG;
     return hip_status(launch_overflow_bound(scale_i32, N, K / group, group, bound_dev, static_cast<hipStream_t>(stream)));
+}
+
+// ---- between a block's projections: per-head norm and rotation, attention, low-rank adapters
+// Rows of `width` elements `ld` apart: 16-byte aligned rows that do not overlap (kMaxLd: a tile's rows keep 32-bit byte offsets).
+static constexpr long long kMaxLd = 1 << 23;
+static bool ok_rows(long long ld, long long width) { return ld >= width && ld % 8 == 0; }
+
+int is_qk_norm_rope(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* gamma_q,
+                    const void* gamma_k, float eps, const float* inv_freq, int rot_dim, int interleaved,
+                    const int32_t* positions, const int64_t* kv_rows, int M, int heads_q, int heads_k, int head_dim,
+                    int64_t cache_rows, void* q_out, int64_t ldqo, void* k_out, int64_t ldko, void* v_out, int64_t ldvo,
+                    void* stream) {
+    if (M < 0 || heads_q < 0 || heads_k < 0 || heads_q + (long long)heads_k < 1 || head_dim <= 0 || rot_dim < 0 || cache_rows < 0)
+        return IS_ERR_INVALID_ARG;
+    if (interleaved != 0 && interleaved != 1) return IS_ERR_INVALID_ARG;
+    if (head_dim % 8 != 0 || rot_dim % 8 != 0 || rot_dim > head_dim) return IS_ERR_INVALID_ARG;
+    if (head_dim > 256 || heads_q > 1024 || heads_k > 1024 || M > (1 << 20)) return IS_ERR_UNSUPPORTED;
+    if ((gamma_q != nullptr || gamma_k != nullptr) && !(eps > 0.0f && eps < INFINITY)) return IS_ERR_INVALID_ARG;
+    if (!ok_opt(gamma_q) || !ok_opt(gamma_k) || (v == nullptr) != (v_out == nullptr)) return IS_ERR_INVALID_ARG;
+    const long long wq = (long long)heads_q * head_dim, wk = (long long)heads_k * head_dim;
+    if (heads_q > 0 && (!ok_rows(ldq, wq) || !ok_rows(ldqo, wq) || (q_out == q && ldqo != ldq))) return IS_ERR_INVALID_ARG;
+    if (heads_k > 0) {
+        if (!ok_rows(ldk, wk) || !ok_rows(ldko, wk) || (k_out == k && ldko != ldk)) return IS_ERR_INVALID_ARG;
+        if (v != nullptr && (!ok_rows(ldv, wk) || !ok_rows(ldvo, wk) || (v_out == v && ldvo != ldv))) return IS_ERR_INVALID_ARG;
+        if (kv_rows == nullptr && cache_rows < M) return IS_ERR_INVALID_ARG;
+        // (in place only onto the same rows: rows that go elsewhere would overwrite ones that are still to be read)
+        if (kv_rows != nullptr && M > 0 && (k_out == k || (v != nullptr && v_out == v))) return IS_ERR_INVALID_ARG;
+    }
+    if (M == 0) return IS_OK;
+    if (positions == nullptr || (reinterpret_cast<uintptr_t>(positions) & 3u) || (reinterpret_cast<uintptr_t>(kv_rows) & 7u))
+        return IS_ERR_INVALID_ARG;
+    if (rot_dim > 0 && (inv_freq == nullptr || (reinterpret_cast<uintptr_t>(inv_freq) & 3u))) return IS_ERR_INVALID_ARG;
+    if (heads_q > 0 && (!ok_ptr(q) || !ok_ptr(q_out))) return IS_ERR_INVALID_ARG;
+    if (heads_k > 0 && (!ok_ptr(k) || !ok_ptr(k_out) || !ok_opt(v) || !ok_opt(v_out))) return IS_ERR_INVALID_ARG;
+    RopeArgs a;
+    a.q = static_cast<const __half*>(q);
+    a.k = static_cast<const __half*>(k);
+    a.v = static_cast<const __half*>(v);
+    a.gamma_q = static_cast<const __half*>(gamma_q);
+    a.gamma_k = static_cast<const __half*>(gamma_k);
+    a.inv_freq = inv_freq;
+    a.positions = positions;
+    a.kv_rows = kv_rows;
+    a.q_out = static_cast<__half*>(q_out);
+    a.k_out = static_cast<__half*>(k_out);
+    a.v_out = static_cast<__half*>(v_out);
+    a.ldq = ldq;
+    a.ldk = ldk;
+    a.ldv = ldv;
+    a.ldqo = ldqo;
+    a.ldko = ldko;
+    a.ldvo = ldvo;
+    a.cache_rows = cache_rows;
+    a.M = M;
+    a.heads_q = heads_q;
+    a.heads_k = heads_k;
+    a.head_dim = head_dim;
+    a.rot_dim = rot_dim;
+    a.eps = eps;
+    a.interleaved = interleaved != 0;
+    return hip_status(launch_qk_norm_rope(a, static_cast<hipStream_t>(stream)));
+}
+
+static int check_attention(int M, int num_seqs, int max_q_len, int max_kv_len, int heads_q, int heads_kv, int head_dim) {
+    if (M < 0 || num_seqs < 0 || max_q_len < 0 || max_kv_len < 0 || heads_q <= 0 || heads_kv <= 0 || head_dim <= 0) return IS_ERR_INVALID_ARG;
+    if (heads_q % heads_kv != 0) return IS_ERR_INVALID_ARG;
+    if (head_dim != 64 && head_dim != 128) return IS_ERR_UNSUPPORTED;
+    if (M > (1 << 20) || heads_q > 1024 || max_kv_len > (1 << 30)) return IS_ERR_UNSUPPORTED;
+    // launch grid: a workgroup per row tile, of which a sequence has at least one, and key head
+    if (((long long)M * (heads_q / heads_kv) / 32 + num_seqs) * heads_kv > (1 << 22)) return IS_ERR_UNSUPPORTED;
+    return IS_OK;
+}
+
+size_t is_attention_workspace_bytes(int M, int num_seqs, int max_q_len, int max_kv_len, int heads_q, int heads_kv, int head_dim) {
+    if (check_attention(M, num_seqs, max_q_len, max_kv_len, heads_q, heads_kv, head_dim) != IS_OK || M == 0 || num_seqs == 0) return 0;
+    return attention_workspace_bytes(attention_plan(M, num_seqs, max_q_len, max_kv_len, heads_kv, heads_q / heads_kv, head_dim), M,
+                                     heads_q, head_dim);
+}
+
+int is_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const int32_t* q_offsets,
+                 const int64_t* kv_starts, const int32_t* kv_lens, int M, int64_t kv_rows, int num_seqs, int max_q_len,
+                 int max_kv_len, int heads_q, int heads_kv, int head_dim, float scale, int causal, void* out, int64_t ldo,
+                 void* workspace, size_t workspace_bytes, void* stream) {
+    const int shape = check_attention(M, num_seqs, max_q_len, max_kv_len, heads_q, heads_kv, head_dim);
+    if (shape != IS_OK) return shape;
+    if (kv_rows < 0 || !(scale > 0.0f && scale < INFINITY) || (causal != 0 && causal != 1)) return IS_ERR_INVALID_ARG;
+    const long long wq = (long long)heads_q * head_dim, wk = (long long)heads_kv * head_dim;
+    if (!ok_rows(ldq, wq) || !ok_rows(ldo, wq) || !ok_rows(ldk, wk) || !ok_rows(ldv, wk)) return IS_ERR_INVALID_ARG;
+    if (ldk > kMaxLd || ldv > kMaxLd) return IS_ERR_UNSUPPORTED;
+    if (!ok_opt(workspace)) return IS_ERR_INVALID_ARG;
+    if (M == 0 || num_seqs == 0) return IS_OK;
+    if (!ok_ptr(q) || !ok_ptr(out) || (kv_rows > 0 && (!ok_ptr(k) || !ok_ptr(v)))) return IS_ERR_INVALID_ARG;
+    if (q_offsets == nullptr || (reinterpret_cast<uintptr_t>(q_offsets) & 3u) || (reinterpret_cast<uintptr_t>(kv_starts) & 7u) ||
+        (reinterpret_cast<uintptr_t>(kv_lens) & 3u))
+        return IS_ERR_INVALID_ARG;
+    const AttnPlan p = attention_plan(M, num_seqs, max_q_len, max_kv_len, heads_kv, heads_q / heads_kv, head_dim);
+    const size_t need = attention_workspace_bytes(p, M, heads_q, head_dim);
+    if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return IS_ERR_WORKSPACE;
+    AttnArgs a;
+    a.q = static_cast<const __half*>(q);
+    a.k = static_cast<const __half*>(k);
+    a.v = static_cast<const __half*>(v);
+    a.out = static_cast<__half*>(out);
+    a.ldq = ldq;
+    a.ldk = ldk;
+    a.ldv = ldv;
+    a.ldo = ldo;
+    a.q_offsets = q_offsets;
+    a.kv_starts = kv_starts;
+    a.kv_lens = kv_lens;
+    a.kv_rows = kv_rows;
+    a.M = M;
+    a.seqs = num_seqs;
+    a.max_q = max_q_len;
+    a.max_kv = max_kv_len;
+    a.heads_kv = heads_kv;
+    a.group = heads_q / heads_kv;
+    a.scale = scale;
+    a.causal = causal != 0;
+    return hip_status(launch_attention(a, p, head_dim, workspace, static_cast<hipStream_t>(stream)));
+}
+
+static int check_lora(int M, int N, int K, int R, int num_adapters) {
+    if (M < 0 || N <= 0 || K <= 0 || R <= 0 || num_adapters < 0 || K % 8 != 0 || R % 8 != 0) return IS_ERR_INVALID_ARG;
+    if (M > (1 << 20) || R > 128 || K > (1 << 20) || N > (1 << 20) || num_adapters > (1 << 20)) return IS_ERR_UNSUPPORTED;
+    return IS_OK;
+}
+
+size_t is_lora_workspace_bytes(int M, int N, int K, int R, int num_adapters) {
+    if (check_lora(M, N, K, R, num_adapters) != IS_OK || M == 0) return 0;
+    return lora_workspace_bytes(M, K, R);
+}
+
+int is_lora_add(const void* x, int64_t ldx, const void* a, const void* b, const int32_t* row_adapter, const float* scales,
+                const int32_t* ranks, int M, int N, int K, int R, int num_adapters, const void* base, int64_t ldb, void* out,
+                int64_t ldo, void* workspace, size_t workspace_bytes, void* stream) {
+    const int shape = check_lora(M, N, K, R, num_adapters);
+    if (shape != IS_OK) return shape;
+    if (!ok_rows(ldx, K) || ldo < N || (base != nullptr && ldb < N) || (base == out && base != nullptr && ldb != ldo)) return IS_ERR_INVALID_ARG;
+    if (!ok_opt(workspace)) return IS_ERR_INVALID_ARG;
+    if (M == 0) return IS_OK;
+    if (!ok_ptr(x) || !ok_ptr(out) || !ok_opt(base) || (num_adapters > 0 && (!ok_ptr(a) || !ok_ptr(b)))) return IS_ERR_INVALID_ARG;
+    if (row_adapter == nullptr || (reinterpret_cast<uintptr_t>(row_adapter) & 3u) || (reinterpret_cast<uintptr_t>(scales) & 3u) ||
+        (reinterpret_cast<uintptr_t>(ranks) & 3u))
+        return IS_ERR_INVALID_ARG;
+    if (workspace == nullptr || workspace_bytes < lora_workspace_bytes(M, K, R)) return IS_ERR_WORKSPACE;
+    LoraArgs l;
+    l.x = static_cast<const __half*>(x);
+    l.a = static_cast<const __half*>(a);
+    l.b = static_cast<const __half*>(b);
+    l.base = static_cast<const __half*>(base);
+    l.row_adapter = row_adapter;
+    l.scales = scales;
+    l.ranks = ranks;
+    l.out = static_cast<__half*>(out);
+    l.ldx = ldx;
+    l.ldb = ldb;
+    l.ldo = ldo;
+    l.M = M;
+    l.N = N;
+    l.K = K;
+    l.R = R;
+    l.adapters = num_adapters;
+    return hip_status(launch_lora_add(l, workspace, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"
