@@ -446,7 +446,8 @@ int is_qk_norm_rope(const void* q, int64_t ldq, const void* k, int64_t ldk, cons
  * Rows of out are written whole; out must not overlap the inputs.  Results do not depend on how a batch's sequences are mixed,
  * but for the split of the keys, which depends on M, num_seqs and the maxima alone.
  * Requirements: head_dim 64 or 128 (IS_ERR_UNSUPPORTED otherwise), heads_kv dividing heads_q, at most 1024 heads, M at most 2^20,
- * max_kv_len at most 2^30, ldk and ldv at most 2^23, (M * g / 32 + num_seqs) * heads_kv at most 2^22; scale positive and finite.
+ * max_kv_len at most 2^30, ldk and ldv at most 2^23, (M * g / 32 + num_seqs) * heads_kv at most 2^22,
+ * num_seqs * (max_kv_len / 32 + 1) below 2^30; scale positive and finite.
  */
 size_t is_attention_workspace_bytes(int M, int num_seqs, int max_q_len, int max_kv_len, int heads_q, int heads_kv, int head_dim);
 int is_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const int32_t* q_offsets,

@@ -1040,13 +1040,16 @@ static int check_attention(int M, int num_seqs, int max_q_len, int max_kv_len, i
     if (M > (1 << 20) || heads_q > 1024 || max_kv_len > (1 << 30)) return IS_ERR_UNSUPPORTED;
     // launch grid: a workgroup per row tile, of which a sequence has at least one, and key head
     if (((long long)M * (heads_q / heads_kv) / 32 + num_seqs) * heads_kv > (1 << 22)) return IS_ERR_UNSUPPORTED;
+    if ((long long)num_seqs * (max_kv_len / 32 + 1) >= (1 << 30)) return IS_ERR_UNSUPPORTED;  // tiles of keys are numbered in 32 bits
     return IS_OK;
 }
 
 size_t is_attention_workspace_bytes(int M, int num_seqs, int max_q_len, int max_kv_len, int heads_q, int heads_kv, int head_dim) {
     if (check_attention(M, num_seqs, max_q_len, max_kv_len, heads_q, heads_kv, head_dim) != IS_OK || M == 0 || num_seqs == 0) return 0;
-    return attention_workspace_bytes(attention_plan(M, num_seqs, max_q_len, max_kv_len, heads_kv, heads_q / heads_kv, head_dim), M,
-                                     heads_q, head_dim);
+    const int group = heads_q / heads_kv;
+    const size_t with = attention_workspace_bytes(attention_plan(M, num_seqs, max_q_len, max_kv_len, heads_kv, group, true), M, heads_kv, group, head_dim);
+    const size_t without = attention_workspace_bytes(attention_plan(M, num_seqs, max_q_len, max_kv_len, heads_kv, group, false), M, heads_kv, group, head_dim);
+    return std::max(with, without);  // (whether the call brings kv_lens is not known here)
 }
 
 int is_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const int32_t* q_offsets,
@@ -1065,8 +1068,8 @@ int is_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const v
     if (q_offsets == nullptr || (reinterpret_cast<uintptr_t>(q_offsets) & 3u) || (reinterpret_cast<uintptr_t>(kv_starts) & 7u) ||
         (reinterpret_cast<uintptr_t>(kv_lens) & 3u))
         return IS_ERR_INVALID_ARG;
-    const AttnPlan p = attention_plan(M, num_seqs, max_q_len, max_kv_len, heads_kv, heads_q / heads_kv, head_dim);
-    const size_t need = attention_workspace_bytes(p, M, heads_q, head_dim);
+    const AttnPlan p = attention_plan(M, num_seqs, max_q_len, max_kv_len, heads_kv, heads_q / heads_kv, kv_lens != nullptr);
+    const size_t need = attention_workspace_bytes(p, M, heads_kv, heads_q / heads_kv, head_dim);
     if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return IS_ERR_WORKSPACE;
     AttnArgs a;
     a.q = static_cast<const __half*>(q);

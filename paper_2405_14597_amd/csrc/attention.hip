@@ -10,6 +10,8 @@
 //
 // Query rows and the query heads of a key head are one axis ("packed rows": row * group + head), so that a tile of 32 packed
 // rows a wave is full for single tokens of grouped heads too and the keys are read once for the whole group.
+#include <algorithm>
+
 #include "block_common.h"
 #include "tile_common.h"
 
@@ -60,8 +62,8 @@ __device__ __forceinline__ Seq seq_at(const AttnArgs& a, int s) {
     return r;
 }
 
-// Which sequence the row tile `target` of the batch belongs to (every sequence has whole tiles of `rows` packed rows) and
-// which of its tiles it is; seq < 0 past the last one.  Each wave by itself, 64 sequences at a time.
+// Which sequence the row tile `target` of the batch belongs to (every sequence of more than few_rows packed rows has whole tiles of
+// `rows`) and which of its tiles it is; seq < 0 past the last one.  Each wave by itself, 64 sequences at a time.
 struct RowTile {
     int seq, tile;
 };
@@ -73,7 +75,8 @@ __device__ __forceinline__ RowTile row_tile(const AttnArgs& a, int target, int r
         int n = 0;
         if (s < a.seqs) {
             const int b = min(max(a.q_offsets[s], 0), a.M), e = min(max(a.q_offsets[s + 1], 0), a.M);
-            n = (max(e - b, 0) * a.group + rows - 1) / rows;
+            const int packed = max(e - b, 0) * a.group;
+            n = packed > a.few_rows ? (packed + rows - 1) / rows : 0;
         }
         const int upto = lanes_up_to(n, lane);
         const unsigned long long past = __ballot(before + upto > target);
@@ -85,6 +88,25 @@ __device__ __forceinline__ RowTile row_tile(const AttnArgs& a, int target, int r
         before += __builtin_amdgcn_readlane(upto, kWave - 1);
     }
     return RowTile{-1, 0};
+}
+
+// Maximum (sum) of a value over the four lanes of equal lane & 15.
+__device__ __forceinline__ float quads_max(float v) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return halves_max(fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1])));
+}
+__device__ __forceinline__ float quads_sum(float v) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return halves_sum(__uint_as_float(s[0]) + __uint_as_float(s[1]));
+}
+
+// Whether an infinity or a NaN is among eight fp16 values in LDS.
+__device__ __forceinline__ bool has_odd_values(LdsPtr p) {
+    const v4i w = *(const __attribute__((address_space(3))) v4i*)p;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) odd = odd || (w[i] & 0x7C00) == 0x7C00 || (w[i] & 0x7C000000) == 0x7C000000;
+    return odd;
 }
 
 // Where 16-byte chunk c of row r of a tile lies in LDS (in chunks from the row's start): rows are a power of two of bytes
@@ -124,7 +146,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2, 2)
     const int rows = s.qlen * a.group;  // packed rows of the sequence
     const int tiles = (rows + NW * kRowsPerWave - 1) / (NW * kRowsPerWave);
     const int first = (tiles - 1 - at.tile) * NW * kRowsPerWave;
-    const int c0 = blockIdx.y * a.chunk;
+    const int c0 = blockIdx.y * a.tile_chunk;
     if (c0 > 0 && c0 >= s.kvlen) return;
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x & (kWave - 1), half = lane >> 5;
@@ -176,7 +198,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2, 2)
     float top = -INFINITY, sum = 0.0f;  // running maximum of scale * q.k (powers of two), sum over this lane's half of the keys
     const float factor = a.scale * 1.44269504088896340736f;
 
-    const int t0 = c0 / kKeys, t1 = (min(c0 + a.chunk, wg_most) + kKeys - 1) / kKeys;
+    const int t0 = c0 / kKeys, t1 = (min(c0 + a.tile_chunk, wg_most) + kKeys - 1) / kKeys;
     if (t0 < t1) fetch(t0, 0);
     for (int t = t0; t < t1; ++t) {
         const int buf = (t - t0) & 1;
@@ -190,11 +212,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2, 2)
         if (min((t + 1) * kKeys, s.kvlen) > wg_least) {
             bool odd = false;
 #pragma unroll
-            for (int i = threadIdx.x * 16; i < kTileBytes; i += NW * kWave * 16) {
-                const v4i w = *(const __attribute__((address_space(3))) v4i*)(vt + i);
-                auto is_odd = [](unsigned x) { return (x & 0x7C00u) == 0x7C00u || (x & 0x7C000000u) == 0x7C000000u; };
-                odd = odd || is_odd(w[0]) || is_odd(w[1]) || is_odd(w[2]) || is_odd(w[3]);
-            }
+            for (int i = threadIdx.x * 16; i < kTileBytes; i += NW * kWave * 16) odd = odd || has_odd_values(vt + i);
             const bool any_odd = __any(odd);
             if (lane == 0) found[buf * NW + wave] = any_odd;
             __syncthreads();
@@ -283,7 +301,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2, 2)
     }
 
     sum = halves_sum(sum);
-    if (s.kvlen <= a.chunk) {
+    if (s.kvlen <= a.tile_chunk) {
         // a row that sees no key is zero; one whose scores are all -inf (or that saw a NaN) is NaN, as the formula's 0 / 0
         const float inv = 1.0f / sum;
         __half* dst = a.out + (size_t)qrow * a.ldo + (size_t)qhead * D;
@@ -315,9 +333,358 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2, 2)
     }
 }
 
+// ---- few rows
+// Sequences of at most kFewRows packed rows (single tokens; the drafts and short chunks of a step): bound by the reading of the
+// keys and values.  Each of a workgroup's waves walks tiles of 32 keys of its own (every NW-th of the chunk's) with a stage of LDS
+// of its own, so that no wave waits for another before the end, where their partial results meet in LDS.  A stage holds one tile
+// of K and one of V: the next K is on its way while the probabilities and the product with V are computed, the next V during the
+// next scores.  The 16-row forms of the matrix instructions, RB times: a group of 4 or 8 heads wastes less of them than of the
+// 32-row ones.
+// As load_to_lds_b128, for bytes that are read once: marked non-temporal they do not push each other through the caches (a decode
+// step of 64 requests, 1.07 GB of keys and values: 198 us without the mark, 176 us with it, 6.1 TB/s).
+__device__ __forceinline__ void stream_to_lds_b128(v4i desc, unsigned lds_base, unsigned lds_offset, int voffset) {
+    asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen nt lds"
+                 :
+                 : "s"(lds_base), "s"(lds_offset), "v"(voffset), "s"(desc)
+                 : "memory", "scc");
+}
+constexpr int kFewKeys = 32;
+constexpr int kFewRows = 64;
+constexpr int few_waves(int rb) { return rb <= 2 ? 8 : 4; }  // (the partial results of 64 rows and eight waves would not fit LDS)
+
+template <int D>
+__device__ __forceinline__ int few_v_chunk(int r, int c) {  // 8 rows, two chunks each
+    return D == 128 ? c ^ ((r & 7) << 1) : c ^ (((r >> 1) & 3) << 1);
+}
+
+// How the tiles of all these sequences are dealt out: numbered from sequence to sequence, every workgroup (and key head) takes the
+// next `per` of them, so that ragged lengths leave nobody idle.  A workgroup's run may end one sequence, hold several whole and begin
+// another; a sequence that lies in one run is finished there, the pieces of the others go to the workspace.
+// Beginning and ending a sequence costs a workgroup about as much as kPiece of its tiles; every sequence counts so many more, in front
+// of its own, so that a run of short ones is no longer than a piece of a long one.
+constexpr int kPiece = 6;
+struct Deal {
+    int per;               // numbers of a workgroup
+    int seq, tiles, begin; // the sequence asked for (seqs: there is none), its tiles, the first number of it
+    Seq s;
+};
+__device__ __forceinline__ int few_tiles(const AttnArgs& a, const Seq& s) {
+    const int rows = s.qlen * a.group;
+    return rows == 0 || rows > a.few_rows ? 0 : max((s.kvlen + kFewKeys - 1) / kFewKeys, 1);  // (rows without keys are written, too)
+}
+// By a wave: sequence `seq`, or (seq < 0) the one that holds the first tile of `slot`.
+__device__ __forceinline__ Deal few_deal(const AttnArgs& a, int slot, int seq) {
+    const int lane = threadIdx.x & (kWave - 1);
+    const Seq none{0, 0, 0, 0};
+    const Seq mine0 = lane < a.seqs ? seq_at(a, lane) : none;
+    auto numbers = [&](const Seq& s) {
+        const int n = few_tiles(a, s);
+        return n > 0 ? n + kPiece : 0;
+    };
+    int total = __builtin_amdgcn_readlane(lanes_up_to(numbers(mine0), lane), kWave - 1);
+    for (int s0 = kWave; s0 < a.seqs; s0 += kWave)
+        total += __builtin_amdgcn_readlane(lanes_up_to(s0 + lane < a.seqs ? numbers(seq_at(a, s0 + lane)) : 0, lane), kWave - 1);
+    Deal d;
+    d.per = max((total + a.slots - 1) / a.slots, a.least_tiles);
+    const long long want = (long long)slot * d.per;
+    int before = 0;
+    for (int s0 = 0; s0 < a.seqs; s0 += kWave) {
+        const Seq mine = s0 == 0 ? mine0 : s0 + lane < a.seqs ? seq_at(a, s0 + lane) : none;
+        const int n = numbers(mine), upto = lanes_up_to(n, lane);
+        const unsigned long long hit = __ballot(seq < 0 ? before + upto > want : s0 + lane == seq);
+        if (hit) {
+            const int at = __builtin_ctzll(hit);
+            d.seq = s0 + at;
+            d.tiles = max(__builtin_amdgcn_readlane(n, at) - kPiece, 0);
+            d.begin = before + __builtin_amdgcn_readlane(upto - n, at);
+            d.s.q0 = __builtin_amdgcn_readlane(mine.q0, at);
+            d.s.qlen = __builtin_amdgcn_readlane(mine.qlen, at);
+            d.s.kvlen = __builtin_amdgcn_readlane(mine.kvlen, at);
+            const unsigned lo = __builtin_amdgcn_readlane((int)mine.kv0, at), hi = __builtin_amdgcn_readlane((int)(mine.kv0 >> 32), at);
+            d.s.kv0 = (long long)(((unsigned long long)hi << 32) | lo);
+            return d;
+        }
+        before += __builtin_amdgcn_readlane(upto, kWave - 1);
+    }
+    d.seq = a.seqs, d.tiles = 0, d.begin = before, d.s = none;
+    return d;
+}
+// Where the piece of a sequence that begins in a run's middle (first: at the sequence's beginning) lies in the workspace, in rows.
+__device__ __forceinline__ size_t piece_at(const AttnArgs& a, int slot, bool first, int head) {
+    return (((size_t)slot * 2 + first) * a.heads_kv + head) * a.few_rows;
+}
+
+template <int D, int RB, int NW>
+__global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(RB * D > 256 ? 1 : 2, 2))) void attention_few_kernel(AttnArgs a) {
+    constexpr int kRowBytes = 2 * D, kTileBytes = kFewKeys * kRowBytes, kLoads = kTileBytes / 1024;
+    constexpr int kSteps = D / 32, kBlocks = D / 16;
+    extern __shared__ __align__(1024) unsigned char lds[];  // [NW][K tile | V tile]; at a piece's end [NW][RB * 16][D] partial results
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x & (kWave - 1), col = lane & 15, quad = lane >> 4;
+    const LdsPtr kt = (LdsPtr)lds + wave * 2 * kTileBytes, vt = kt + kTileBytes;
+    const unsigned kt_base = (unsigned)(uintptr_t)(LdsPtr)lds + wave * 2 * kTileBytes;
+    float* part = reinterpret_cast<float*>(lds);                          // [NW][RB * 16][D], columns rotated by the row
+    float2* ml = reinterpret_cast<float2*>(lds + NW * RB * 16 * D * 4);   // [NW][RB * 16]
+
+    // (heads side by side: with 8 or 32 of them the workgroups i, i + 8, ... of an XCD read the same heads' columns; the heads of a run
+    // on one XCD instead read 1.2 GB in 183 us where this takes 176)
+    const int slot = blockIdx.x / a.heads_kv, head = blockIdx.x % a.heads_kv;
+    const Deal deal = few_deal(a, slot, -1);
+    int seq = deal.seq, tiles = deal.tiles, begin = deal.begin, at = slot * deal.per;
+    const int end = at + deal.per;
+    Seq s = deal.s;
+
+    int k_off[kLoads], v_off[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+        const int byte = j * 1024 + lane * 16, r = byte / kRowBytes, c = byte % kRowBytes / 16;
+        k_off[j] = r * (int)(a.ldk * 2) + k_chunk<D>(r, c) * 16;
+        v_off[j] = r * (int)(a.ldv * 2) + few_v_chunk<D>(r, c) * 16;
+    }
+    const float factor = a.scale * 1.44269504088896340736f;
+
+    while (seq < a.seqs && at < end) {
+    if (at == begin && seq != deal.seq) {
+        s = seq_at(a, seq);
+        tiles = few_tiles(a, s);
+        if (tiles == 0) {
+            ++seq;
+            continue;
+        }
+    }
+    const int rows = s.qlen * a.group;
+    const int t0 = max(at - begin - kPiece, 0), t1 = min(end - begin - kPiece, tiles);
+    if (t1 <= t0) break;  // (the run ends in front of the sequence's first tile)
+    const bool whole = t0 == 0 && t1 == tiles;
+
+    int lim[RB];
+    h8 q[RB][kSteps];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+        const int p = b * 16 + col, row = p / a.group;
+        const bool mine = p < rows;
+        lim[b] = !mine ? 0 : a.causal ? max(min(row + s.kvlen - s.qlen + 1, s.kvlen), 0) : s.kvlen;
+        const __half* src = a.q + (size_t)(s.q0 + (mine ? row : 0)) * a.ldq + (size_t)(head * a.group + (mine ? p - row * a.group : 0)) * D + quad * 8;
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) q[b][kk] = mine ? *reinterpret_cast<const h8*>(src + kk * 32) : h8{};
+    }
+    const int least = a.causal ? max(s.kvlen - s.qlen + 1, 0) : s.kvlen;  // keys that every row sees
+    const __half* k_head = a.k + (size_t)s.kv0 * a.ldk + (size_t)head * D;
+    const __half* v_head = a.v + (size_t)s.kv0 * a.ldv + (size_t)head * D;
+    auto fetch = [&](const __half* base, long long ld, int t, const int (&off)[kLoads], unsigned to) {
+        const int left = min(s.kvlen - t * kFewKeys, kFewKeys);  // (rows past the sequence's last read as zero)
+        const v4i d = make_desc(base + (size_t)t * kFewKeys * ld, left > 0 ? (size_t)(left - 1) * ld * 2 + kRowBytes : 0);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) stream_to_lds_b128(d, to, j * 1024, off[j]);
+    };
+
+    v4f o[RB][kBlocks];
+    float top[RB], sum[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+        top[b] = -INFINITY, sum[b] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) o[b][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    int t = t0 + wave;
+    if (t < t1) {
+        fetch(k_head, a.ldk, t, k_off, kt_base);
+        fetch(v_head, a.ldv, t, v_off, kt_base + kTileBytes);
+    }
+    for (; t < t1; t += NW) {
+        const bool more = t + NW < t1;
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");  // K is here, V may be on its way
+        v4f sc[RB][2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+#pragma unroll
+            for (int b = 0; b < RB; ++b) sc[b][m] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            const int r = m * 16 + col;
+#pragma unroll
+            for (int kk = 0; kk < kSteps; ++kk) {
+                const h8 kv = lds_h8(kt + r * kRowBytes + k_chunk<D>(r, 4 * kk + quad) * 16);
+#pragma unroll
+                for (int b = 0; b < RB; ++b) sc[b][m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv, q[b][kk], sc[b][m], 0, 0, 0);
+            }
+        }
+        // (the next tile's loads write where this one was read: the reads have to be over)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) fetch(k_head, a.ldk, t + NW, k_off, kt_base);
+        h8 pr[RB];
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            const int seen = lim[b] - t * kFewKeys - 4 * quad;  // element i of block m: key 16 m + 4 quad + i
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = sc[b][i / 4][i % 4];
+            if ((t + 1) * kFewKeys > least) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = 16 * (i / 4) + i % 4 < seen ? x[i] : -INFINITY;
+            }
+            float most = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+            most = quads_max(most) * factor;
+            if (__any(most > top[b] + kLazyMax)) {
+                const float now = fmaxf(top[b], most);
+                const float shrink = now == -INFINITY ? 1.0f : exp2_fast(top[b] - now);
+#pragma unroll
+                for (int i = 0; i < kBlocks; ++i) o[b][i] *= shrink;
+                sum[b] *= shrink;
+                top[b] = now;
+            }
+            const float less = top[b] == -INFINITY ? 0.0f : top[b];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float p = exp2_fast(fmaf(x[i], factor, -less));
+                sum[b] += p;
+                pr[b][i] = (_Float16)p;
+            }
+        }
+        if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        bool odd = false;  // (keys that only some rows see, as in the kernel above)
+        if (min((t + 1) * kFewKeys, s.kvlen) > least) {
+#pragma unroll
+            for (int i = 0; i < kTileBytes; i += 1024) odd = odd || has_odd_values(vt + i + lane * 16);
+            odd = __any(odd);
+        }
+        auto values = [&](int i) {  // V^T: column 16 i + (lane & 15), keys 4 quad + 0..3 and those 16 further on
+            const int r = 4 * quad + (col >> 2), c = 2 * i + (col >> 1 & 1);
+            const h4 x = lds_h4_turned(vt + r * kRowBytes + few_v_chunk<D>(r, c) * 16 + (col & 1) * 8);
+            const h4 y = lds_h4_turned(vt + (r + 16) * kRowBytes + few_v_chunk<D>(r + 16, c) * 16 + (col & 1) * 8);
+            return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        if (!odd) {
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i) {
+                const h8 v = values(i);
+#pragma unroll
+                for (int b = 0; b < RB; ++b) o[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pr[b], o[b][i], 0, 0, 0);
+            }
+        } else {
+#pragma unroll 1
+            for (int key = 0; key < kFewKeys; ++key) {
+                const int e = (key / 16) * 4 + key % 4;
+                const bool here = (key / 4 & 3) == quad;
+#pragma unroll
+                for (int i = 0; i < kBlocks; ++i) {
+                    h8 v = values(i);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = j == e && here ? v[j] : (_Float16)0.0f;
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) {
+                        h8 pk;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) pk[j] = j == e && here ? pr[b][j] : (_Float16)0.0f;
+                        const v4f one = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pk, v4f{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) o[b][i][j] = t * kFewKeys + key < lim[b] ? o[b][i][j] + one[j] : o[b][i][j];
+                    }
+                }
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) fetch(v_head, a.ldv, t + NW, v_off, kt_base + kTileBytes);
+    }
+
+    // ---- the waves' results: lane's row 16 b + col, columns 16 i + 4 quad + 0..3
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+        sum[b] = quads_sum(sum[b]);
+        const int r = b * 16 + col;
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i)
+            *reinterpret_cast<v4f*>(part + (size_t)(wave * RB * 16 + r) * D + ((16 * i + 4 * quad + 4 * col) & (D - 1))) = o[b][i];
+        if (quad == 0) ml[wave * RB * 16 + r] = make_float2(top[b], sum[b]);
+    }
+    __syncthreads();
+    constexpr int kFours = RB * 16 * D / 4;
+#pragma unroll
+    for (int at = threadIdx.x; at < kFours; at += NW * kWave) {
+        const int r = at / (D / 4), c = at % (D / 4) * 4;
+        if (r >= rows) continue;
+        float most = ml[r].x;
+#pragma unroll
+        for (int w = 1; w < NW; ++w) most = fmaxf(most, ml[w * RB * 16 + r].x);
+        const float less = most == -INFINITY ? 0.0f : most;
+        v4f acc = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        float total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float2 m = ml[w * RB * 16 + r];
+            const float f = exp2_fast(m.x - less);
+            total = fmaf(m.y, f, total);
+            acc += f * *reinterpret_cast<const v4f*>(part + (size_t)(w * RB * 16 + r) * D + ((c + 4 * (r & 15)) & (D - 1)));
+        }
+        if (whole) {
+            const int row = r / a.group, seen = a.causal ? row + s.kvlen - s.qlen + 1 : s.kvlen;
+            h4 y;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = seen > 0 ? (_Float16)(acc[j] / total) : (_Float16)0.0f;
+            *reinterpret_cast<h4*>(a.out + (size_t)(s.q0 + row) * a.ldo + (size_t)(head * a.group + (r - row * a.group)) * D + c) = y;
+        } else {
+            const size_t to = piece_at(a, slot, t0 == 0, head) + r;
+            *reinterpret_cast<v4f*>(a.few_o + to * D + c) = acc;
+            if (c == 0) a.few_ml[to] = make_float2(most, total);
+        }
+    }
+    __syncthreads();  // (the next piece's tiles go where the partial results were)
+    begin += kPiece + tiles;
+    at = begin;
+    ++seq;
+    }
+}
+
+// The pieces of a sequence that several workgroups had, joined in their order: a workgroup for each sequence and key head.
+template <int D>
+__global__ __launch_bounds__(256) void attention_few_join_kernel(AttnArgs a) {
+    const int seq = blockIdx.x / a.heads_kv, head = blockIdx.x % a.heads_kv;
+    const Deal d = few_deal(a, 0, seq);
+    if (d.tiles == 0) return;
+    const int first = (d.begin + kPiece) / d.per, last = (d.begin + kPiece + d.tiles - 1) / d.per;
+    if (first == last) return;  // (written already)
+    const Seq s = d.s;
+    const int rows = s.qlen * a.group;
+    for (int i = threadIdx.x; i < rows * (D / 4); i += 256) {
+        const int r = i / (D / 4), c = i % (D / 4) * 4;
+        float top = -INFINITY, sum = 0.0f;
+        v4f acc = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        constexpr int kAtOnce = 8;
+        for (int p0 = first; p0 <= last; p0 += kAtOnce) {
+            float2 m[kAtOnce];
+            v4f v[kAtOnce];
+            float now = top;
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                const int p = min(p0 + j, last);
+                const size_t from = piece_at(a, p, p == first, head) + r;
+                m[j] = a.few_ml[from];
+                v[j] = *reinterpret_cast<const v4f*>(a.few_o + from * D + c);
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) now = fmaxf(now, m[j].x);
+            const float less = now == -INFINITY ? 0.0f : now, shrink = exp2_fast(top - less);
+            sum *= shrink;
+            acc *= shrink;
+            top = now;
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j)
+                if (p0 + j <= last) {
+                    const float f = exp2_fast(m[j].x - less);
+                    sum = fmaf(m[j].y, f, sum);
+                    acc += f * v[j];
+                }
+        }
+        const int row = r / a.group, seen = a.causal ? row + s.kvlen - s.qlen + 1 : s.kvlen;
+        h4 y;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = seen > 0 ? (_Float16)(acc[j] / sum) : (_Float16)0.0f;
+        *reinterpret_cast<h4*>(a.out + (size_t)(s.q0 + row) * a.ldo + (size_t)(head * a.group + (r - row * a.group)) * D + c) = y;
+    }
+}
+
 // The chunks' partial results of a row and head, joined in the chunks' order: one wave each.
 template <int D>
-__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256) void attention_tile_join_kernel(AttnArgs a) {
     const int lane = threadIdx.x & (kWave - 1);
     const int heads = a.heads_kv * a.group;
     const long long at = (long long)blockIdx.x * 4 + threadIdx.x / kWave;
@@ -336,21 +703,42 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
     }
     if (seq < 0) return;
     const Seq s = seq_at(a, seq);
-    if (s.kvlen <= a.chunk) return;  // (written already)
-    const int chunks = (s.kvlen + a.chunk - 1) / a.chunk;
+    const int chunk = a.tile_chunk;
+    if (s.qlen * a.group <= a.few_rows || s.kvlen <= chunk) return;  // (not this kernel's, or written already)
+    const int chunks = (s.kvlen + chunk - 1) / chunk;
+    // the chunks' maxima and sums lie in the lanes, the partial rows come eight at a time
     const size_t stride = (size_t)a.M * heads;
-    float top = -INFINITY;
-    for (int c = 0; c < chunks; ++c) top = fmaxf(top, a.part_ml[c * stride + at].x);
-    const float less = top == -INFINITY ? 0.0f : top;
-    constexpr int E = D / kWave;
-    float acc[E] = {}, sum = 0.0f;
-    for (int c = 0; c < chunks; ++c) {
-        const float2 ml = a.part_ml[c * stride + at];
-        const float w = exp2_fast(ml.x - less);
-        sum = fmaf(ml.y, w, sum);
-        const float* src = a.part_o + (c * stride + at) * D + lane * E;
+    constexpr int E = D / kWave, kAtOnce = 8;
+    float acc[E] = {}, sum = 0.0f, top = -INFINITY;
+    for (int c0 = 0; c0 < chunks; c0 += kWave) {
+        const int n = min(chunks - c0, kWave);
+        const float2 ml = lane < n ? a.part_ml[(size_t)(c0 + lane) * stride + at] : make_float2(-INFINITY, 0.0f);
+        float now = ml.x;
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = fmaf(src[e], w, acc[e]);
+        for (int d = 1; d < 16; d *= 2) now = fmaxf(now, __shfl_xor(now, d, kWave));
+        now = fmaxf(quads_max(now), top);
+        const float less = now == -INFINITY ? 0.0f : now, shrink = exp2_fast(top - less), w = exp2_fast(ml.x - less);
+        top = now;
+        float part = ml.y * w;
+#pragma unroll
+        for (int d = 1; d < 16; d *= 2) part += __shfl_xor(part, d, kWave);
+        sum = fmaf(sum, shrink, quads_sum(part));
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] *= shrink;
+        const float* src = a.part_o + ((size_t)c0 * stride + at) * D + lane * E;
+        for (int c = 0; c < n; c += kAtOnce) {
+            float v[kAtOnce][E];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[i][e] = src[(size_t)min(c + i, n - 1) * stride * D + e];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), min(c + i, n - 1)));
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] = c + i < n ? fmaf(v[i][e], f, acc[e]) : acc[e];
+            }
+        }
     }
     const int lim = a.causal ? row - s.q0 + s.kvlen - s.qlen + 1 : s.kvlen;
     __half* dst = a.out + (size_t)row * a.ldo + (size_t)head * D + lane * E;
@@ -360,6 +748,22 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
 
 constexpr int kTileWaves = 8;
 
+inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+template <int D, int RB>
+hipError_t launch_few(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
+    constexpr int NW = few_waves(RB), stages = NW * 2 * kFewKeys * 2 * D, parts = NW * RB * 16 * (4 * D + 8), bytes = stages > parts ? stages : parts;
+    static LdsLimit limit;
+    const auto kernel = attention_few_kernel<D, RB, NW>;
+    const hipError_t e = limit.raise(reinterpret_cast<const void*>(kernel));
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.slots * a.heads_kv)), dim3(NW * kWave), bytes, stream, a);
+    const hipError_t launched = hipGetLastError();
+    if (launched != hipSuccess || !p.few_cut) return launched;
+    hipLaunchKernelGGL((attention_few_join_kernel<D>), dim3((unsigned)(a.seqs * a.heads_kv)), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
 template <int D>
 hipError_t launch_tiles(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
     constexpr int bytes = 4 * kKeys * 2 * D + 2 * kTileWaves * 4;
@@ -368,46 +772,75 @@ hipError_t launch_tiles(const AttnArgs& a, const AttnPlan& p, hipStream_t stream
     const hipError_t e = limit.raise(reinterpret_cast<const void*>(kernel));
     if (e != hipSuccess) return e;
     const long long tiles = (long long)a.M * a.group / (kTileWaves * kRowsPerWave) + a.seqs;  // no fewer than the sequences' whole tiles
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles * a.heads_kv), p.chunks), dim3(kTileWaves * kWave), bytes, stream, a);
-    const hipError_t launched = hipGetLastError();
-    if (launched != hipSuccess || p.chunks == 1) return launched;
-    const long long waves = (long long)a.M * a.heads_kv * a.group;
-    hipLaunchKernelGGL((attention_join_kernel<D>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles * a.heads_kv), p.tile_chunks), dim3(kTileWaves * kWave), bytes, stream, a);
     return hipGetLastError();
 }
 
-inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+template <int D>
+hipError_t launch_all(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
+    hipError_t e = hipSuccess;
+    if (p.tiles) e = launch_tiles<D>(a, p, stream);
+    if (e != hipSuccess) return e;
+    if (p.few_rows > 0) e = p.few_rows <= 16 ? launch_few<D, 1>(a, p, stream) : p.few_rows <= 32 ? launch_few<D, 2>(a, p, stream) : launch_few<D, 4>(a, p, stream);
+    if (e != hipSuccess || p.tile_chunks == 1) return e;
+    const long long waves = (long long)a.M * a.heads_kv * a.group;
+    hipLaunchKernelGGL((attention_tile_join_kernel<D>), dim3((unsigned)ceil_div(waves, 4)), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+// Keys to a workgroup: all of them, or so many that the chip gets `want` workgroups, a multiple of `step` and no fewer than `least`.
+void cut_keys(int max_kv, long long workgroups, int want, int step, int least, int* chunk, int* chunks) {
+    const long long pieces = want / (workgroups < 1 ? 1 : workgroups);
+    const long long whole = ceil_div(max_kv < 1 ? 1 : max_kv, step) * step;
+    long long keys = pieces > 1 ? ceil_div(ceil_div(max_kv, pieces), step) * step : whole;
+    if (keys < least) keys = least;
+    if (keys > whole) keys = whole;
+    *chunk = (int)keys;
+    *chunks = (int)ceil_div(whole, keys);
+}
 
 }  // namespace
 
-// Keys are cut into chunks where the row tiles alone would leave most of the units idle.
-AttnPlan attention_plan(int M, int seqs, int max_q, int max_kv, int heads_kv, int group, int head_dim) {
-    const int whole = (int)ceil_div(max_kv, kKeys) * kKeys;
-    AttnPlan p{whole > 0 ? whole : kKeys, 1};
-    const long long rows = kTileWaves * kRowsPerWave;
-    const long long tiles = ((long long)M * group / rows + seqs) * heads_kv;
-    const long long want = 2LL * cu_count() / tiles;
-    if (want > 1) {
-        const long long chunk = ceil_div(ceil_div(max_kv, want), kKeys) * kKeys;
-        p.chunk = (int)(chunk < 256 ? 256 : chunk);
-        p.chunks = (int)ceil_div(max_kv, p.chunk);
-        if (p.chunks < 1) p.chunks = 1;
+AttnPlan attention_plan(int M, int seqs, int max_q, int max_kv, int heads_kv, int group, bool own_lens) {
+    AttnPlan p;
+    const long long most = (long long)max_q * group;
+    const int singles = group <= 16 ? 16 : group <= 32 ? 32 : group <= kFewRows ? kFewRows : 0;
+    p.tiles = most > kFewRows;
+    // beside longer sequences the kernel for few rows takes single tokens; there are none where all are equally long, and without
+    // lengths of their own their keys are as few as their rows
+    if (!p.tiles) p.few_rows = most <= 16 ? 16 : most <= 32 ? 32 : kFewRows;
+    else p.few_rows = own_lens && M < (long long)seqs * max_q ? singles : 0;
+    if (p.few_rows > 0) {
+        // One workgroup a unit, none with less than 18 tiles (576 keys) of a sequence.
+        constexpr int kLeast = 18 + kPiece;
+        const long long most = ceil_div(max_kv < 1 ? 1 : max_kv, kFewKeys) + kPiece;  // numbers of a sequence
+        p.least_tiles = kLeast;
+        p.slots = (int)std::min(ceil_div(cu_count(), heads_kv), ceil_div(seqs * most, kLeast));
+        p.few_cut = p.slots > 1 && (seqs > 1 || most > kLeast);
     }
+    if (p.tiles) cut_keys(max_kv, ((long long)M * group / (kTileWaves * kRowsPerWave) + 1) * heads_kv, 2 * cu_count(), kKeys, 256, &p.tile_chunk, &p.tile_chunks);
     return p;
 }
 
-size_t attention_workspace_bytes(const AttnPlan& p, int M, int heads_q, int head_dim) {
-    return p.chunks == 1 ? 0 : (size_t)p.chunks * M * heads_q * (head_dim * 4 + 8);
+static size_t few_part_rows(const AttnPlan& p, int heads_kv) { return p.few_cut ? (size_t)p.slots * 2 * heads_kv * p.few_rows : 0; }
+static size_t tile_part_rows(const AttnPlan& p, int M, int heads_q) { return p.tile_chunks == 1 ? 0 : (size_t)p.tile_chunks * M * heads_q; }
+
+size_t attention_workspace_bytes(const AttnPlan& p, int M, int heads_kv, int group, int head_dim) {
+    return (few_part_rows(p, heads_kv) + tile_part_rows(p, M, heads_kv * group)) * (head_dim * 4 + 8);
 }
 
 hipError_t launch_attention(const AttnArgs& args, const AttnPlan& p, int head_dim, void* workspace, hipStream_t stream) {
     AttnArgs a = args;
-    a.chunk = p.chunk;
-    if (p.chunks > 1) {
-        a.part_o = static_cast<float*>(workspace);
-        a.part_ml = reinterpret_cast<float2*>(a.part_o + (size_t)p.chunks * a.M * a.heads_kv * a.group * head_dim);
-    }
-    return head_dim == 128 ? launch_tiles<128>(a, p, stream) : launch_tiles<64>(a, p, stream);
+    a.few_rows = p.few_rows;
+    a.slots = p.slots;
+    a.least_tiles = p.least_tiles;
+    a.tile_chunk = p.tile_chunk;
+    const size_t few = few_part_rows(p, a.heads_kv), tile = tile_part_rows(p, a.M, a.heads_kv * a.group);
+    a.few_o = static_cast<float*>(workspace);
+    a.part_o = a.few_o + few * head_dim;
+    a.few_ml = reinterpret_cast<float2*>(a.part_o + tile * head_dim);
+    a.part_ml = a.few_ml + few;
+    return head_dim == 128 ? launch_all<128>(a, p, stream) : launch_all<64>(a, p, stream);
 }
 
 }  // namespace intscale

@@ -34,16 +34,23 @@ struct AttnArgs {
     float scale;
     bool causal;
     // set by the launcher
-    int chunk = 0;                   // keys of a workgroup (a multiple of 64)
-    float* part_o = nullptr;         // [chunk index][M * query heads][head_dim], unnormalised
-    float2* part_ml = nullptr;       // [chunk index][M * query heads]: maximum (in powers of two) and sum
+    int few_rows = 0;                // sequences of no more packed rows (rows * group) take the kernel for few rows
+    int slots = 0, least_tiles = 0;  // its workgroups for each key head, and the fewest tiles of one
+    float* few_o = nullptr;          // [slot][2][key head][few_rows][head_dim], unnormalised
+    float2* few_ml = nullptr;        // [slot][2][key head][few_rows]: maximum (in powers of two) and sum
+    int tile_chunk = 0;              // keys of a row tile's workgroup
+    float* part_o = nullptr;         // [chunk index][M * query heads][head_dim]
+    float2* part_ml = nullptr;       // [chunk index][M * query heads]
 };
-// Keys of a workgroup's chunk and the number of chunks of the longest sequence; > 1: partial results in the workspace.
 struct AttnPlan {
-    int chunk, chunks;
+    bool tiles = false;              // sequences of more than few_rows packed rows are expected
+    int tile_chunk = 0, tile_chunks = 1;  // keys of a row tile's workgroup, chunks of the longest sequence
+    int few_rows = 0;                // 0: the kernel for few rows is not launched
+    int slots = 0, least_tiles = 0;
+    bool few_cut = false;            // a sequence may lie in several workgroups' runs
 };
-AttnPlan attention_plan(int M, int seqs, int max_q, int max_kv, int heads_kv, int group, int head_dim);
-size_t attention_workspace_bytes(const AttnPlan& p, int M, int heads_q, int head_dim);
+AttnPlan attention_plan(int M, int seqs, int max_q, int max_kv, int heads_kv, int group, bool own_lens);
+size_t attention_workspace_bytes(const AttnPlan& p, int M, int heads_kv, int group, int head_dim);
 hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, int head_dim, void* workspace, hipStream_t stream);
 
 struct LoraArgs {
