@@ -1103,7 +1103,7 @@ static int check_lora(int M, int N, int K, int R, int num_adapters) {
 
 size_t is_lora_workspace_bytes(int M, int N, int K, int R, int num_adapters) {
     if (check_lora(M, N, K, R, num_adapters) != IS_OK || M == 0) return 0;
-    return lora_workspace_bytes(M, K, R);
+    return lora_workspace_bytes(M, N, K, R);
 }
 
 int is_lora_add(const void* x, int64_t ldx, const void* a, const void* b, const int32_t* row_adapter, const float* scales,
@@ -1118,7 +1118,7 @@ int is_lora_add(const void* x, int64_t ldx, const void* a, const void* b, const 
     if (row_adapter == nullptr || (reinterpret_cast<uintptr_t>(row_adapter) & 3u) || (reinterpret_cast<uintptr_t>(scales) & 3u) ||
         (reinterpret_cast<uintptr_t>(ranks) & 3u))
         return IS_ERR_INVALID_ARG;
-    if (workspace == nullptr || workspace_bytes < lora_workspace_bytes(M, K, R)) return IS_ERR_WORKSPACE;
+    if (workspace == nullptr || workspace_bytes < lora_workspace_bytes(M, N, K, R)) return IS_ERR_WORKSPACE;
     LoraArgs l;
     l.x = static_cast<const __half*>(x);
     l.a = static_cast<const __half*>(a);

@@ -64,8 +64,7 @@ struct LoraArgs {
     float* inner = nullptr;          // workspace: [slab][M][R] sums of x a^T over a slab of K
     int slabs = 1;
 };
-int lora_slabs(int M, int K);
-size_t lora_workspace_bytes(int M, int K, int R);
+size_t lora_workspace_bytes(int M, int N, int K, int R);
 hipError_t launch_lora_add(const LoraArgs& a, void* workspace, hipStream_t stream);
 
 }  // namespace intscale

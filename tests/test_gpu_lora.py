@@ -47,7 +47,10 @@ def check(got, ref, what):
 @pytest.mark.parametrize("M,N,K,R,E,mix", [
     (1, 1024, 4096, 8, 4, 2), (1, 1, 8, 8, 1, 0), (16, 64, 136, 16, 3, "rows"), (17, 100, 4096, 16, 20, "rows"), (64, 4096, 4096, 16, 32, "rows"),
     (5, 5003, 256, 64, 2, "rows"), (100, 257, 1000, 24, 5, "runs"), (300, 384, 520, 128, 7, "runs"), (33, 72, 40, 40, 6, "rows"),
-    (1000, 136, 264, 32, 3, "runs"), (40, 48, 64, 8, 2, -1), (40, 48, 64, 8, 2, 2), (2000, 96, 128, 96, 1, 0)])
+    (1000, 136, 264, 32, 3, "runs"), (40, 48, 64, 8, 2, -1), (40, 48, 64, 8, 2, 2), (2000, 96, 128, 96, 1, 0),
+    # from 2^26 products of the wider side on: by tiles
+    (1101, 1003, 72, 64, 5, "runs"), (530, 256, 2056, 64, 3, "rows"), (4207, 1000, 40, 16, 9, "runs"), (1050, 520, 1000, 128, 2, "runs"),
+    (2100, 2008, 8, 24, 1, -1), (1800, 1168, 96, 40, 40, "rows"), (4097, 2049, 64, 8, 2, 1)])
 def test_against_oracle(M, N, K, R, E, mix):
     print("lora", M, N, K, R, E, mix, flush=True)
     c = make(M, N, K, R, E, M + N + K, mix)
@@ -66,24 +69,29 @@ def test_against_oracle(M, N, K, R, E, mix):
         check(part, (ref[0][keep.numpy()], ref[1][keep.numpy()]), "every second row")
 
 
-def test_strides_and_what_lies_between():
-    c = make(50, 90, 64, 16, 3, 9, "rows")
+FORMS = pytest.mark.parametrize("M,N,R", [(50, 90, 16), (2100, 1002, 32), (2100, 1000, 32)], ids=["rows", "tiles", "tiles_wide"])
+
+
+@FORMS
+def test_strides_and_what_lies_between(M, N, R):
+    c = make(M, N, 64, R, 3, 9, "rows")
     d = on(c)
-    x = torch.full((50, 96), float("nan"), dtype=torch.float16, device=DEV)
+    x = torch.full((M, 96), float("nan"), dtype=torch.float16, device=DEV)
     x[:, 16:80] = d["x"]
-    wide = torch.full((50, 131), 7.0, dtype=torch.float16, device=DEV)
-    wide[:, :90] = d["base"]
-    y = wide[:, :90]
+    wide = torch.full((M, N + (41 if M == 50 else 40)), 7.0, dtype=torch.float16, device=DEV)
+    wide[:, :N] = d["base"]
+    y = wide[:, :N]
     P.is_lora_add(x[:, 16:80], d["a"], d["b"], d["e"], y, scales=d["scales"], ranks=d["ranks"], out=y)
     check(y, want(c), "strided")
-    assert (wide[:, 90:] == 7).all()
+    assert (wide[:, N:] == 7).all()
 
 
-def test_nothing_of_another_adapter_reaches_a_row():
+@FORMS
+def test_nothing_of_another_adapter_reaches_a_row(M, N, R):
     # NaN and infinities in adapters, ranks' rests and rows of other requests
-    c = make(48, 80, 72, 16, 4, 11, "rows")
-    c["ranks"] = torch.tensor([16, 5, 16, 9], dtype=torch.int32)
-    c["e"] = torch.randint(0, 4, (48,), generator=torch.Generator().manual_seed(2), dtype=torch.int32)
+    c = make(M, N, 72, R, 4, 11, "rows")
+    c["ranks"] = torch.tensor([R, 5, R, 9], dtype=torch.int32)
+    c["e"] = torch.randint(0, 4, (M,), generator=torch.Generator().manual_seed(2), dtype=torch.int32)
     ref = want(c)
     c["a"][2], c["b"][2] = float("inf"), float("nan")
     for e in (1, 3):
@@ -98,9 +106,10 @@ def test_nothing_of_another_adapter_reaches_a_row():
     assert torch.isnan(got[5]).all() and not torch.isfinite(got[odd.to(DEV)]).any()
 
 
-def test_large_inner_products():
+@FORMS
+def test_large_inner_products(M, N, R):
     # x a^T far past fp16's largest number, b small: the output is ordinary
-    c = make(20, 64, 512, 16, 2, 13, "rows")
+    c = make(M, N, 512, R, 2, 13, "rows")
     c["x"], c["a"], c["b"] = c["x"] * 400, (c["a"].float() * 400).half(), (c["b"].float() * 2e-6).half()
     d = on(c)
     assert (c["x"].float() @ c["a"][0].float().t()).abs().max() > 1e6
