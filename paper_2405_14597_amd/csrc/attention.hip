@@ -109,6 +109,20 @@ __device__ __forceinline__ bool has_odd_values(LdsPtr p) {
     return odd;
 }
 
+// Sets the infinities and NaN among eight fp16 values in LDS to zero; whether there were any.
+__device__ __forceinline__ bool take_out_odd_values(LdsPtr p) {
+    v4i w = *(const __attribute__((address_space(3))) v4i*)p;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool low = (w[i] & 0x7C00) == 0x7C00, high = (w[i] & 0x7C000000) == 0x7C000000;
+        w[i] &= (low ? 0 : 0xFFFF) | (high ? 0 : (int)0xFFFF0000);
+        odd = odd || low || high;
+    }
+    if (odd) *(__attribute__((address_space(3))) v4i*)p = w;
+    return odd;
+}
+
 // Where 16-byte chunk c of row r of a tile lies in LDS (in chunks from the row's start): rows are a power of two of bytes
 // apart, so without it the rows that one read touches would meet in the same banks.
 template <int D>
@@ -128,7 +142,9 @@ __device__ __forceinline__ h4 lds_h4_turned(LdsPtr p) {
 
 // One workgroup: NW waves of 32 packed rows of one sequence and key head, one chunk of its keys.  Grid: x = key head +
 // heads_kv * row tile (the key heads of a row tile go to different XCDs, and with 8 of them one head's keys stay in one
-// XCD's L2), y = chunk.  The last row tile of a sequence, which sees the most keys, comes first.
+// XCD's L2), y = chunk.  The last row tile of a sequence, which sees the most keys, comes first.  (All sequences' last tiles before
+// anybody's others: 84 us instead of 72 for five sequences both ways, 1185 instead of 1137 for a prompt of 8192.)  Four waves, two
+// workgroups a unit: a prompt of 8192 rows and 64 heads 1137 us (967 TFLOP/s), 1172 with eight waves, whose barrier holds all of a unit's.
 template <int D, int NW>
 __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void attention_tile_kernel(AttnArgs a) {
     constexpr int kRowBytes = 2 * D, kTileBytes = kKeys * kRowBytes, kLoads = kTileBytes / 1024 / NW;
@@ -207,33 +223,35 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2, 2)
         if (t + 1 < t1) fetch(t + 1, buf ^ 1);
         const LdsPtr kt = lds_p + buf * 2 * kTileBytes, vt = kt + kTileBytes;
         // Keys that some rows see and others do not: a product with a probability of zero still turns an infinity or a NaN among
-        // their values into a NaN, so such a tile is looked through first.
+        // their values into a NaN.  Such a tile is looked through first, and those values are taken out; the rows that see them get
+        // them below.
         bool odd_values = false;
         if (min((t + 1) * kKeys, s.kvlen) > wg_least) {
             bool odd = false;
 #pragma unroll
-            for (int i = threadIdx.x * 16; i < kTileBytes; i += NW * kWave * 16) odd = odd || has_odd_values(vt + i);
+            for (int i = threadIdx.x * 16; i < kTileBytes; i += NW * kWave * 16) odd = take_out_odd_values(vt + i) || odd;
             const bool any_odd = __any(odd);
-            if (lane == 0) found[buf * NW + wave] = any_odd;
+            if (lane == 0) found[(t & 1) * NW + wave] = any_odd;
             __syncthreads();
 #pragma unroll
-            for (int w = 0; w < NW; ++w) odd_values = odd_values || found[buf * NW + w];
+            for (int w = 0; w < NW; ++w) odd_values = odd_values || found[(t & 1) * NW + w];
         }
         if (t * kKeys >= w_most) continue;  // (wave-uniform: no row of this wave sees the tile)
 
         f16v sc[2];
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
+        for (int i = 0; i < 32; ++i) sc[i / 16][i % 16] = 0.0f;
+        // (the two blocks of 32 keys in turn: two products in a row into the same accumulators would wait for each other)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[m][i] = 0.0f;
-            const int r = m * 32 + (lane & 31);
+        for (int kk = 0; kk < kSteps; ++kk)
 #pragma unroll
-            for (int kk = 0; kk < kSteps; ++kk)
-                sc[m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds_h8(kt + r * kRowBytes + k_chunk<D>(r, 2 * kk + half) * 16), q[kk],
-                                                               sc[m], 0, 0, 0);
-        }
+            for (int m = 0; m < 2; ++m) {
+                const int r = m * 32 + (lane & 31);
+                sc[m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds_h8(kt + r * kRowBytes + k_chunk<D>(r, 2 * kk + half) * 16), q[kk], sc[m], 0, 0, 0);
+            }
         const int seen = lim - t * kKeys - 4 * half;  // element i of block m: key m * 32 + 8 * (i / 4) + i % 4 of this half
         if ((t + 1) * kKeys > w_least) {
+            asm volatile("");  // (a branch: as selects in every tile these would be a sixth of its instructions)
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -271,30 +289,22 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2, 2)
             const h4 y = lds_h4_turned(vt + (r + 8) * kRowBytes + v_chunk<D>(r + 8, c >> 4) * 16 + (c & 15));
             return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
         };
-        if (!odd_values) {
 #pragma unroll
-            for (int step = 0; step < 4; ++step)
+        for (int step = 0; step < 4; ++step)
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(values(step, b), pr[step], o[b], 0, 0, 0);
-        } else {  // key by key, and only into the rows that see it
+            for (int b = 0; b < kBlocks; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(values(step, b), pr[step], o[b], 0, 0, 0);
+        if (odd_values) {  // what was taken out, to the rows that see it (a probability is positive: times it, it stays what it is)
 #pragma unroll 1
-            for (int key = 0; key < kKeys; ++key) {
-                const int step = key / 16, h = key / 4 & 1, e = (key / 8 & 1) * 4 + key % 4;
-                h8 pk = step == 0 ? pr[0] : step == 1 ? pr[1] : step == 2 ? pr[2] : pr[3];
+            for (int key = t * kKeys; key < min((t + 1) * kKeys, s.kvlen); ++key) {
+                const __half* src = v_head + (size_t)key * a.ldv + 4 * half;
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b) {
-                    h8 v = values(step, b);
+                for (int i = 0; i < 16 * kBlocks; i += 4) {
+                    const h4 v = *reinterpret_cast<const h4*>(src + 2 * i);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        if (j != e || h != half) v[j] = (_Float16)0.0f;
-                        if (j != e || h != half) pk[j] = (_Float16)0.0f;
+                    for (int j = 0; j < 4; ++j) {
+                        const float x = (float)v[j];
+                        if (key < lim && !(fabsf(x) < INFINITY)) o[i / 16][i % 16 + j] += x;
                     }
-                    f16v one;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) one[i] = 0.0f;
-                    one = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pk, one, 0, 0, 0);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[b][i] = t * kKeys + key < lim ? o[b][i] + one[i] : o[b][i];
                 }
             }
         }
@@ -746,7 +756,7 @@ __global__ __launch_bounds__(256) void attention_tile_join_kernel(AttnArgs a) {
     for (int e = 0; e < E; ++e) dst[e] = __float2half(lim > 0 ? acc[e] / sum : 0.0f);
 }
 
-constexpr int kTileWaves = 8;
+constexpr int kTileWaves = 4;
 
 inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
