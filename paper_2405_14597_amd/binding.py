@@ -1095,26 +1095,35 @@ def is_linear_w4a8_floatscale_prepacked(x, packed: PackedWeights, out=None, work
 # --------------------------------------------------------------------------------------------------------------
 # Between a block's projections: per-head norm and rotation, attention, low-rank adapters
 # --------------------------------------------------------------------------------------------------------------
-def _rows(t, shape, device, name) -> int:
-    """fp16 rows that may lie apart (columns of a wider buffer); returns how many elements lie between their beginnings."""
-    if t.dtype != _torch().float16 or t.shape != shape or (t.shape[1] > 1 and t.stride(1) != 1) or t.get_device() != device:
-        raise ValueError(f"{name}: expected a cuda tensor of float16 rows {tuple(shape)} on device {device}, got {t.dtype} "
-                         f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
-    return t.stride(0) if shape[0] > 1 else -(-shape[1] // 8) * 8
-
-
-def _vector(t, dtype, n, device, name) -> None:
-    if t is not None and (t.dtype != dtype or t.shape != (n,) or not t.is_contiguous() or t.get_device() != device):
-        raise ValueError(f"{name}: expected contiguous cuda tensor {dtype} ({n},) on device {device}, got {t.dtype} {tuple(t.shape)} "
-                         f"on {t.device}")
+# (these checks run on every call of a decode step: few attribute reads each, the constants looked up once)
+_half_dtype = _int32_dtype = _int64_dtype = _float_dtype = None
 
 
 def _device_of(t, name) -> int:
     """The device of a call's tensors, which has to be the current one: the call's stream belongs to that."""
-    device = t.get_device() if t.is_cuda else -1
-    if device < 0 or device != _torch().cuda.current_device():
+    global _half_dtype, _int32_dtype, _int64_dtype, _float_dtype
+    if _half_dtype is None:
+        torch = _torch()
+        _half_dtype, _int32_dtype, _int64_dtype, _float_dtype = torch.float16, torch.int32, torch.int64, torch.float32
+    device = t.get_device()
+    if device < 0 or device != (_current_device or _torch().cuda.current_device)():
         raise ValueError(f"{name}: expected a tensor on the current cuda device, got one on {t.device}")
     return device
+
+
+def _rows(t, rows, width, device, name) -> int:
+    """fp16 rows that may lie apart (columns of a wider buffer); returns how many elements lie between their beginnings."""
+    ld, step = t.stride() if t.dim() == 2 else (0, 0)
+    if t.dtype is not _half_dtype or t.shape != (rows, width) or (step != 1 and width > 1) or t.get_device() != device:
+        raise ValueError(f"{name}: expected a cuda tensor of float16 rows {(rows, width)} on device {device}, got {t.dtype} "
+                         f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    return ld if rows > 1 else -(-width // 8) * 8
+
+
+def _vector(t, dtype, n, device, name) -> None:
+    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{name}: expected contiguous cuda tensor {dtype} ({n},) on device {device}, got {t.dtype} {tuple(t.shape)} "
+                         f"on {t.device}")
 
 
 def is_qk_norm_rope(q, k, positions, inv_freq, head_dim: int, gamma_q=None, gamma_k=None, eps: float = 1e-5, interleaved: bool = False,
@@ -1123,7 +1132,6 @@ def is_qk_norm_rope(q, k, positions, inv_freq, head_dim: int, gamma_q=None, gamm
     their first 2 * inv_freq.numel() columns a head.  With kv_rows (int64 [M]) the keys and the values v go to those rows of
     the caches k_out and v_out.  q_out = q (and without kv_rows k_out = k, v_out = v) works in place.
     Returns (q_out, k_out), with v (q_out, k_out, v_out)."""
-    torch = _torch()
     device = _device_of(q, "q")
     M, wq = q.shape
     wk = k.shape[1]
@@ -1133,23 +1141,29 @@ def is_qk_norm_rope(q, k, positions, inv_freq, head_dim: int, gamma_q=None, gamm
         raise ValueError("kv_rows: the caches that they are rows of are k_out (and v_out)")
     if v is None and v_out is not None:
         raise ValueError("v_out: there is no v")
-    q_out = torch.empty((M, wq), dtype=torch.float16, device=q.device) if q_out is None else q_out
-    k_out = torch.empty((M, wk), dtype=torch.float16, device=q.device) if k_out is None else k_out
+    if q_out is None:
+        q_out = _torch().empty((M, wq), dtype=_half_dtype, device=q.device)
+    if k_out is None:
+        k_out = _torch().empty((M, wk), dtype=_half_dtype, device=q.device)
     if v is not None and v_out is None:
-        v_out = torch.empty((M, wk), dtype=torch.float16, device=q.device)
+        v_out = _torch().empty((M, wk), dtype=_half_dtype, device=q.device)
     rows = k_out.shape[0] if kv_rows is not None else M
-    ldq, ldk = _rows(q, (M, wq), device, "q"), _rows(k, (M, wk), device, "k")
-    ldqo, ldko = _rows(q_out, (M, wq), device, "q_out"), _rows(k_out, (rows, wk), device, "k_out")
+    ldq, ldk = _rows(q, M, wq, device, "q"), _rows(k, M, wk, device, "k")
+    ldqo, ldko = _rows(q_out, M, wq, device, "q_out"), _rows(k_out, rows, wk, device, "k_out")
     ldv = ldvo = 0
     if v is not None:
-        ldv, ldvo = _rows(v, (M, wk), device, "v"), _rows(v_out, (rows, wk), device, "v_out")
-    _vector(positions, torch.int32, M, device, "positions")
-    _vector(inv_freq, torch.float32, inv_freq.numel(), device, "inv_freq")
-    _vector(kv_rows, torch.int64, M, device, "kv_rows")
-    _vector(gamma_q, torch.float16, head_dim, device, "gamma_q")
-    _vector(gamma_k, torch.float16, head_dim, device, "gamma_k")
+        ldv, ldvo = _rows(v, M, wk, device, "v"), _rows(v_out, rows, wk, device, "v_out")
+    pairs = inv_freq.numel()
+    _vector(positions, _int32_dtype, M, device, "positions")
+    _vector(inv_freq, _float_dtype, pairs, device, "inv_freq")
+    if kv_rows is not None:
+        _vector(kv_rows, _int64_dtype, M, device, "kv_rows")
+    if gamma_q is not None:
+        _vector(gamma_q, _half_dtype, head_dim, device, "gamma_q")
+    if gamma_k is not None:
+        _vector(gamma_k, _half_dtype, head_dim, device, "gamma_k")
     st = load_library().is_qk_norm_rope(_p(q), ldq, _p(k), ldk, _p(v), ldv, _p(gamma_q), _p(gamma_k), eps, _p(inv_freq),
-                                        2 * inv_freq.numel(), int(interleaved), _p(positions), _p(kv_rows), M, wq // head_dim,
+                                        2 * pairs, int(interleaved), _p(positions), _p(kv_rows), M, wq // head_dim,
                                         wk // head_dim, head_dim, rows, _p(q_out), ldqo, _p(k_out), ldko, _p(v_out), ldvo,
                                         _stream_handle(stream))
     _check("is_qk_norm_rope", st)
@@ -1165,7 +1179,6 @@ def is_attention(q, k, v, q_offsets, head_dim: int, max_q_len: int, max_kv_len: 
     """Attention of the packed sequences q [M, heads * head_dim] over k, v [rows, kv heads * head_dim]: sequence s has the rows
     q_offsets[s] .. q_offsets[s + 1] of q and, of k and v, kv_lens[s] rows from kv_starts[s] on (without them the same rows as of q).
     scale: head_dim ** -0.5 if not given.  Returns out [M, heads * head_dim]; rows of no sequence stay as they are (zero in a new one)."""
-    torch = _torch()
     device = _device_of(q, "q")
     M, wq = q.shape
     rows, wk = k.shape
@@ -1173,12 +1186,14 @@ def is_attention(q, k, v, q_offsets, head_dim: int, max_q_len: int, max_kv_len: 
     if head_dim <= 0 or wq % head_dim or wk % head_dim:
         raise ValueError(f"q, k: {wq} and {wk} columns are no whole heads of {head_dim}")
     if out is None:
-        out = torch.zeros((M, wq), dtype=torch.float16, device=q.device)
-    ldq, ldo = _rows(q, (M, wq), device, "q"), _rows(out, (M, wq), device, "out")
-    ldk, ldv = _rows(k, (rows, wk), device, "k"), _rows(v, (rows, wk), device, "v")
-    _vector(q_offsets, torch.int32, seqs + 1, device, "q_offsets")
-    _vector(kv_starts, torch.int64, seqs, device, "kv_starts")
-    _vector(kv_lens, torch.int32, seqs, device, "kv_lens")
+        out = _torch().zeros((M, wq), dtype=_half_dtype, device=q.device)
+    ldq, ldo = _rows(q, M, wq, device, "q"), _rows(out, M, wq, device, "out")
+    ldk, ldv = _rows(k, rows, wk, device, "k"), _rows(v, rows, wk, device, "v")
+    _vector(q_offsets, _int32_dtype, seqs + 1, device, "q_offsets")
+    if kv_starts is not None:
+        _vector(kv_starts, _int64_dtype, seqs, device, "kv_starts")
+    if kv_lens is not None:
+        _vector(kv_lens, _int32_dtype, seqs, device, "kv_lens")
     sizes = (M, seqs, max_q_len, max_kv_len, wq // head_dim, wk // head_dim, head_dim)
     ws, ws_bytes = _workspace(is_attention_workspace_bytes, sizes, q.device, workspace)
     st = load_library().is_attention(_p(q), ldq, _p(k), ldk, _p(v), ldv, _p(q_offsets), _p(kv_starts), _p(kv_lens), M, rows, seqs, max_q_len,
@@ -1197,22 +1212,23 @@ def is_lora_add(x, a, b, row_adapter, base, scales=None, ranks=None, out=None, w
     """base [M, N] plus the low-rank adapters' share of x [M, K]: adapter e = row_adapter[m] (none outside 0 .. E - 1) adds
     scales[e] * (x[m] a[e]^T) b[e]^T with a [E, R, K], b [E, N, R], of which ranks[e] of R count.  base None: zeros; out = base
     works in place.  Returns out [M, N]."""
-    torch = _torch()
     device = _device_of(x, "x")
     M, K = x.shape
     E, R, _ = a.shape
     N = b.shape[1]
-    _require(a, torch.float16, (E, R, K), "a")
-    _require(b, torch.float16, (E, N, R), "b")
+    _require(a, _half_dtype, (E, R, K), "a")
+    _require(b, _half_dtype, (E, N, R), "b")
     if a.get_device() != device or b.get_device() != device:
         raise ValueError(f"a, b: expected tensors on device {device}")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=x.device)
-    ldx, ldo = _rows(x, (M, K), device, "x"), _rows(out, (M, N), device, "out")
-    ldb = _rows(base, (M, N), device, "base") if base is not None else 0
-    _vector(row_adapter, torch.int32, M, device, "row_adapter")
-    _vector(scales, torch.float32, E, device, "scales")
-    _vector(ranks, torch.int32, E, device, "ranks")
+        out = _torch().empty((M, N), dtype=_half_dtype, device=x.device)
+    ldx, ldo = _rows(x, M, K, device, "x"), _rows(out, M, N, device, "out")
+    ldb = _rows(base, M, N, device, "base") if base is not None else 0
+    _vector(row_adapter, _int32_dtype, M, device, "row_adapter")
+    if scales is not None:
+        _vector(scales, _float_dtype, E, device, "scales")
+    if ranks is not None:
+        _vector(ranks, _int32_dtype, E, device, "ranks")
     ws, ws_bytes = _workspace(is_lora_workspace_bytes, (M, N, K, R, E), x.device, workspace)
     st = load_library().is_lora_add(_p(x), ldx, _p(a), _p(b), _p(row_adapter), _p(scales), _p(ranks), M, N, K, R, E, _p(base), ldb, _p(out),
                                     ldo, _p(ws), ws_bytes, _stream_handle(stream))

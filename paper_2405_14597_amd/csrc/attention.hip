@@ -63,31 +63,55 @@ __device__ __forceinline__ Seq seq_at(const AttnArgs& a, int s) {
 }
 
 // Which sequence the row tile `target` of the batch belongs to (every sequence of more than few_rows packed rows has whole tiles of
-// `rows`) and which of its tiles it is; seq < 0 past the last one.  Each wave by itself, 64 sequences at a time.
+// `rows`) and which of its tiles it is; seq < 0 past the last one.  Each wave by itself.  Up to 64 sequences the longest come
+// first, or the last workgroups to start would be the longest ones (twelve prompts of 17 to 2048 rows: 177 us in the batch's order,
+// 172 so); one sequence after the other, since their keys and values stay in the caches that way.
 struct RowTile {
     int seq, tile;
+    Seq s;
 };
+__device__ __forceinline__ int row_tiles(const AttnArgs& a, const Seq& s, int rows) {
+    const int packed = s.qlen * a.group;
+    return packed > a.few_rows ? (packed + rows - 1) / rows : 0;
+}
+// The sequence that lane `at` has, to all lanes.
+__device__ __forceinline__ Seq seq_of_lane(const Seq& mine, int at) {
+    Seq s;
+    s.q0 = __builtin_amdgcn_readlane(mine.q0, at);
+    s.qlen = __builtin_amdgcn_readlane(mine.qlen, at);
+    s.kvlen = __builtin_amdgcn_readlane(mine.kvlen, at);
+    const unsigned lo = __builtin_amdgcn_readlane((int)mine.kv0, at), hi = __builtin_amdgcn_readlane((int)(mine.kv0 >> 32), at);
+    s.kv0 = (long long)(((unsigned long long)hi << 32) | lo);
+    return s;
+}
 __device__ __forceinline__ RowTile row_tile(const AttnArgs& a, int target, int rows) {
     const int lane = threadIdx.x & (kWave - 1);
+    const Seq none{0, 0, 0, 0};
+    if (a.seqs <= kWave) {
+        const Seq mine = lane < a.seqs ? seq_at(a, lane) : none;
+        const int n = row_tiles(a, mine, rows);
+        int before = 0;
+        for (int s = 0; s < a.seqs; ++s) {
+            const int other = __builtin_amdgcn_readlane(n, s);
+            before += other > n || (other == n && s < lane) ? other : 0;
+        }
+        const unsigned long long here = __ballot(target >= before && target < before + n);
+        if (here == 0) return RowTile{-1, 0, none};
+        const int at = __builtin_ctzll(here);
+        return RowTile{at, target - __builtin_amdgcn_readlane(before, at), seq_of_lane(mine, at)};
+    }
     int before = 0;
     for (int s0 = 0; s0 < a.seqs; s0 += kWave) {
-        const int s = s0 + lane;
-        int n = 0;
-        if (s < a.seqs) {
-            const int b = min(max(a.q_offsets[s], 0), a.M), e = min(max(a.q_offsets[s + 1], 0), a.M);
-            const int packed = max(e - b, 0) * a.group;
-            n = packed > a.few_rows ? (packed + rows - 1) / rows : 0;
-        }
-        const int upto = lanes_up_to(n, lane);
+        const Seq mine = s0 + lane < a.seqs ? seq_at(a, s0 + lane) : none;
+        const int n = row_tiles(a, mine, rows), upto = lanes_up_to(n, lane);
         const unsigned long long past = __ballot(before + upto > target);
         if (past) {
             const int first = __builtin_ctzll(past);
-            const int skipped = before + __builtin_amdgcn_readlane(upto - n, first);
-            return RowTile{s0 + first, target - skipped};
+            return RowTile{s0 + first, target - before - __builtin_amdgcn_readlane(upto - n, first), seq_of_lane(mine, first)};
         }
         before += __builtin_amdgcn_readlane(upto, kWave - 1);
     }
-    return RowTile{-1, 0};
+    return RowTile{-1, 0, none};
 }
 
 // Maximum (sum) of a value over the four lanes of equal lane & 15.
@@ -146,7 +170,7 @@ __device__ __forceinline__ h4 lds_h4_turned(LdsPtr p) {
 // anybody's others: 84 us instead of 72 for five sequences both ways, 1185 instead of 1137 for a prompt of 8192.)  Four waves, two
 // workgroups a unit: a prompt of 8192 rows and 64 heads 1137 us (967 TFLOP/s), 1172 with eight waves, whose barrier holds all of a unit's.
 template <int D, int NW>
-__global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void attention_tile_kernel(AttnArgs a) {
+__global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2))) void attention_tile_kernel(AttnArgs a) {
     constexpr int kRowBytes = 2 * D, kTileBytes = kKeys * kRowBytes, kLoads = kTileBytes / 1024 / NW;
     constexpr int kSteps = D / 16, kBlocks = D / 32;
     static_assert(kLoads >= 1, "every wave loads a part of a tile");
@@ -158,7 +182,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2, 2)
     const int head = blockIdx.x % a.heads_kv;
     const RowTile at = row_tile(a, blockIdx.x / a.heads_kv, NW * kRowsPerWave);
     if (at.seq < 0) return;
-    const Seq s = seq_at(a, at.seq);
+    const Seq s = at.s;
     const int rows = s.qlen * a.group;  // packed rows of the sequence
     const int tiles = (rows + NW * kRowsPerWave - 1) / (NW * kRowsPerWave);
     const int first = (tiles - 1 - at.tile) * NW * kRowsPerWave;
@@ -175,13 +199,6 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2, 2)
     const bool mine = p < rows;
     const int lim = mine ? limit(p) : 0;
     const int qrow = s.q0 + (mine ? p / a.group : 0), qhead = head * a.group + (mine ? p % a.group : 0);
-
-    h8 q[kSteps];
-    {
-        const __half* src = a.q + (size_t)qrow * a.ldq + (size_t)qhead * D + half * 8;
-#pragma unroll
-        for (int kk = 0; kk < kSteps; ++kk) q[kk] = mine ? *reinterpret_cast<const h8*>(src + kk * 16) : h8{};
-    }
 
     // a tile's rows to LDS: kilobyte i of the tile is wave i / kLoads's, its rows' chunks permuted on the way
     int k_off[kLoads], v_off[kLoads];
@@ -216,6 +233,12 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2, 2)
 
     const int t0 = c0 / kKeys, t1 = (min(c0 + a.tile_chunk, wg_most) + kKeys - 1) / kKeys;
     if (t0 < t1) fetch(t0, 0);
+    h8 q[kSteps];
+    {
+        const __half* src = a.q + (size_t)qrow * a.ldq + (size_t)qhead * D + half * 8;
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) q[kk] = mine ? *reinterpret_cast<const h8*>(src + kk * 16) : h8{};
+    }
     for (int t = t0; t < t1; ++t) {
         const int buf = (t - t0) & 1;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -407,11 +430,7 @@ __device__ __forceinline__ Deal few_deal(const AttnArgs& a, int slot, int seq) {
             d.seq = s0 + at;
             d.tiles = max(__builtin_amdgcn_readlane(n, at) - kPiece, 0);
             d.begin = before + __builtin_amdgcn_readlane(upto - n, at);
-            d.s.q0 = __builtin_amdgcn_readlane(mine.q0, at);
-            d.s.qlen = __builtin_amdgcn_readlane(mine.qlen, at);
-            d.s.kvlen = __builtin_amdgcn_readlane(mine.kvlen, at);
-            const unsigned lo = __builtin_amdgcn_readlane((int)mine.kv0, at), hi = __builtin_amdgcn_readlane((int)(mine.kv0 >> 32), at);
-            d.s.kv0 = (long long)(((unsigned long long)hi << 32) | lo);
+            d.s = seq_of_lane(mine, at);
             return d;
         }
         before += __builtin_amdgcn_readlane(upto, kWave - 1);
