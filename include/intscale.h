@@ -441,10 +441,12 @@ int is_qk_norm_rope(const void* q, int64_t ldq, const void* k, int64_t ldk, cons
  *   kv_starts    int64 [num_seqs] or NULL: the sequence's first row of k and v (NULL: q_offsets[s]).  Sequences may share rows.
  *   kv_lens      int32 [num_seqs] or NULL: its number of keys (NULL: its number of rows of q).  A sequence whose start lies outside
  *                [0, kv_rows] has none; one that runs over the end of k and v ends there.
- *   max_q_len, max_kv_len   no sequence is longer (they choose the kernel and the split of the keys; keys past max_kv_len are left out)
- *   workspace    at least is_attention_workspace_bytes(...) bytes (0 when the keys are not split), contents arbitrary
+ *   max_q_len, max_kv_len   no sequence is longer (they choose the kernels and the split of the keys; rows of a sequence of more than
+ *                max_q_len may be left as they are, keys past max_kv_len are left out)
+ *   workspace    at least is_attention_workspace_bytes(...) bytes (0 when the keys are not split), contents arbitrary; calls that
+ *                share one must not overlap in time
  * Rows of out are written whole; out must not overlap the inputs.  Results do not depend on how a batch's sequences are mixed,
- * but for the split of the keys, which depends on M, num_seqs and the maxima alone.
+ * but for the split of the keys, which follows from the batch's sizes and lengths: the same call gives the same bits.
  * Requirements: head_dim 64 or 128 (IS_ERR_UNSUPPORTED otherwise), heads_kv dividing heads_q, at most 1024 heads, M at most 2^20,
  * max_kv_len at most 2^30, ldk and ldv at most 2^23, (M * g / 32 + num_seqs) * heads_kv at most 2^22,
  * num_seqs * (max_kv_len / 32 + 1) below 2^30; scale positive and finite.
@@ -464,8 +466,9 @@ int is_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const v
  *   row_adapter  int32 [M];  scales  float [num_adapters] or NULL (1);  ranks  int32 [num_adapters] or NULL (R): what lies past an
  *                adapter's rank (rows of a, columns of b) does not count
  *   base, out    fp16 [M] rows of N elements, ldb and ldo apart.  base is the projection's output (NULL: zeros); out may be base
- *                (ldo = ldb; rows without an adapter are then left alone)
- *   workspace    at least is_lora_workspace_bytes(...) bytes, contents arbitrary
+ *                (ldo = ldb; rows without an adapter are then left alone); out overlaps
+ *                no other argument
+ *   workspace    at least is_lora_workspace_bytes(...) bytes, contents arbitrary; calls that share one must not overlap in time
  * Requirements: K and R multiples of 8, R at most 128, ldx a multiple of 8; M, N, K and num_adapters at most 2^20.
  */
 size_t is_lora_workspace_bytes(int M, int N, int K, int R, int num_adapters);

@@ -832,6 +832,7 @@ void cut_keys(int max_kv, long long workgroups, int want, int step, int least, i
 
 AttnPlan attention_plan(int M, int seqs, int max_q, int max_kv, int heads_kv, int group, bool own_lens) {
     AttnPlan p;
+    max_q = std::min(max_q, M);
     const long long most = (long long)max_q * group;
     const int singles = group <= 16 ? 16 : group <= 32 ? 32 : group <= kFewRows ? kFewRows : 0;
     p.tiles = most > kFewRows;

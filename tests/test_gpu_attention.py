@@ -86,6 +86,48 @@ def test_many_sequences():
         check(run(c, causal), oracle(c, causal), causal)
 
 
+@pytest.mark.parametrize("hq,hk,d", [(64, 1, 128), (65, 1, 64), (16, 1, 128), (4, 4, 128)])
+def test_groups_at_the_kernels_limits(hq, hk, d):
+    # packed rows of a token at and past what the kernel for few rows takes; drafts of a few tokens; loose maxima
+    for seqs in ([(1, 900), (1, 33)], [(2, 700), (4, 64), (1, 1)]):
+        c = make(seqs, hq, hk, d, hq + d, gap=2)
+        ref = oracle(c, True)
+        check(run(c, True), ref, seqs)
+        check(run(c, True, max_q_len=4096, max_kv_len=100000), ref, "loose")
+
+
+def test_ragged_decode_batch_over_many_workgroups():
+    # more than a wave of sequences whose keys are dealt out over workgroups that begin and end inside them
+    g = np.random.default_rng(5)
+    seqs = [(1, int(n)) for n in np.exp(g.uniform(0, np.log(4000), 90))]
+    seqs[40], seqs[41], seqs[42] = (0, 3000), (1, 0), (1, 9000)
+    c = make(seqs, 2, 1, 128, 61, gap=5)
+    check(run(c, True), oracle(c, True), "90 sequences")
+    c = make(seqs[:64], 2, 1, 64, 62)
+    check(run(c, False), oracle(c, False), "64 sequences")
+    # beside prompts
+    c = make(seqs[:20] + [(70, 300), (150, 150)] + seqs[50:60], 4, 2, 128, 63, gap=1)
+    check(run(c, True), oracle(c, True), "beside prompts")
+
+
+def test_two_calls_at_once():
+    # on two streams, each with its own workspace
+    c, d = make([(1, 5000), (1, 77)], 8, 2, 128, 68), make([(60, 1000), (1, 2000)], 8, 2, 128, 69)
+    want = [run(x, True) for x in (c, d)]
+    whole = lambda v, t: torch.tensor(v, dtype=t, device=DEV)  # noqa: E731
+    streams, args = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for x in (c, d):
+        args.append((x["q"].to(DEV), x["k"].to(DEV), x["v"].to(DEV), whole(x["off"], torch.int32), 128, x["mq"], x["mkv"], whole(x["starts"], torch.int64),
+                     whole(x["lens"], torch.int32), torch.zeros(tuple(x["q"].shape), dtype=torch.float16, device=DEV)))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, (q, k, v, off, hd, mq, mkv, starts, lens, out) in zip(streams, args):
+            with torch.cuda.stream(s):
+                P.is_attention(q, k, v, off, hd, mq, mkv, kv_starts=starts, kv_lens=lens, out=out)
+    torch.cuda.synchronize()
+    assert torch.equal(args[0][-1], want[0]) and torch.equal(args[1][-1], want[1])
+
+
 def test_scale_and_large_scores():
     # scores of some hundreds: one key takes nearly all, the maximum moves far and often
     c = make([(40, 300), (1, 900)], 4, 2, 128, 23)
@@ -181,16 +223,17 @@ def test_offsets_past_32_bits():
 
 
 def test_shared_rows_and_the_order_of_sequences():
-    # two sequences over the same prefix; the batch in another order gives the same bits
+    # two sequences over the same prefix; the batch in another order; the same call gives the same bits
     c = make([(1, 600), (1, 550), (20, 400)], 8, 2, 128, 53)
     c["starts"][1] = c["starts"][0]
-    a = run(c, True)
-    check(a, oracle(c, True), "shared")
+    a, ref = run(c, True), oracle(c, True)
+    check(a, ref, "shared")
+    assert torch.equal(a, run(c, True))
     perm = [2, 0, 1]
     rows = [list(range(c["off"][s], c["off"][s + 1])) for s in perm]
     b = run({**c, "q": c["q"][sum(rows, [])], "off": np.cumsum([0] + [len(r) for r in rows]).tolist(), "starts": [c["starts"][s] for s in perm],
              "lens": [c["lens"][s] for s in perm]}, True)
-    assert torch.equal(b, a[sum(rows, [])])
+    check(b, (ref[0][sum(rows, [])], ref[1][sum(rows, [])]), "another order")
 
 
 def test_captured_calls_replay():
