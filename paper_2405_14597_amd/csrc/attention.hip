@@ -238,6 +238,10 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2))) 
         const __half* src = a.q + (size_t)qrow * a.ldq + (size_t)qhead * D + half * 8;
 #pragma unroll
         for (int kk = 0; kk < kSteps; ++kk) q[kk] = mine ? *reinterpret_cast<const h8*>(src + kk * 16) : h8{};
+        // Used here, so that they are waited for here: waited for at their first use in the loop, every tile would wait for the
+        // next one's loads as well.
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) asm volatile("" : "+v"(q[kk]));
     }
     for (int t = t0; t < t1; ++t) {
         const int buf = (t - t0) & 1;
@@ -272,6 +276,15 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2))) 
                 const int r = m * 32 + (lane & 31);
                 sc[m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds_h8(kt + r * kRowBytes + k_chunk<D>(r, 2 * kk + half) * 16), q[kk], sc[m], 0, 0, 0);
             }
+        // six (four) reads ahead of the products: two at a time would leave each pair of products waiting for LDS
+        constexpr int kAhead = D == 128 ? 6 : 4;
+        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < (2 * kSteps - kAhead) / 2; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
         const int seen = lim - t * kKeys - 4 * half;  // element i of block m: key m * 32 + 8 * (i / 4) + i % 4 of this half
         if ((t + 1) * kKeys > w_least) {
             asm volatile("");  // (a branch: as selects in every tile these would be a sixth of its instructions)
@@ -519,6 +532,11 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(RB * 
         fetch(k_head, a.ldk, t, k_off, kt_base);
         fetch(v_head, a.ldv, t, v_off, kt_base + kTileBytes);
     }
+    // (used here to be waited for here: at their first use in the loop, K would wait for V as well)
+#pragma unroll
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) asm volatile("" : "+v"(q[b][kk]));
     for (; t < t1; t += NW) {
         const bool more = t + NW < t1;
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");  // K is here, V may be on its way
