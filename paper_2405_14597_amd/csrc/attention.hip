@@ -10,6 +10,12 @@
 //
 // Query rows and the query heads of a key head are one axis ("packed rows": row * group + head), so that a tile of 32 packed
 // rows a wave is full for single tokens of grouped heads too and the keys are read once for the whole group.
+//
+// Two kernels: row tiles (prompts and chunks of them), bound by the matrix instructions, the exponentials beside them and what of both does
+// not overlap (8192 rows, 64 heads of 128: 1076 to 1135 us from box to box, 0.97 to 1.02 PFLOP/s; counters: matrix pipe busy 38 % of the time, vector
+// instructions 40 %, LDS 19 %, no bank conflicts, 2.0 GHz); few rows (single tokens), bound by memory (64 requests, 1.07 GB: 171 us, 6.2 TB/s;
+// a plain streaming read 6.4).  Not kept for row tiles: the next tile's scores under this tile's probabilities (24 to 84 registers spilled at
+// heads of 128, 1450 us and more; no gain at heads of 64), wave priorities (no change).
 #include <algorithm>
 
 #include "block_common.h"
@@ -167,8 +173,9 @@ __device__ __forceinline__ h4 lds_h4_turned(LdsPtr p) {
 // One workgroup: NW waves of 32 packed rows of one sequence and key head, one chunk of its keys.  Grid: x = key head +
 // heads_kv * row tile (the key heads of a row tile go to different XCDs, and with 8 of them one head's keys stay in one
 // XCD's L2), y = chunk.  The last row tile of a sequence, which sees the most keys, comes first.  (All sequences' last tiles before
-// anybody's others: 84 us instead of 72 for five sequences both ways, 1185 instead of 1137 for a prompt of 8192.)  Four waves, two
-// workgroups a unit: a prompt of 8192 rows and 64 heads 1137 us (967 TFLOP/s), 1172 with eight waves, whose barrier holds all of a unit's.
+// anybody's others: 84 us instead of 72 for five sequences both ways, 4 % more for a prompt of 8192.)  Four waves, two workgroups a unit
+// (heads of 64: three): with eight waves, whose barrier holds all of a unit's, a prompt of 8192 rows takes 1 % less, five sequences both ways
+// 74 us instead of 61, a chunk of 300 rows beside 24 requests 119 instead of 106.
 template <int D, int NW>
 __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2))) void attention_tile_kernel(AttnArgs a) {
     constexpr int kRowBytes = 2 * D, kTileBytes = kKeys * kRowBytes, kLoads = kTileBytes / 1024 / NW;
@@ -387,7 +394,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2))) 
 // next scores.  The 16-row forms of the matrix instructions, RB times: a group of 4 or 8 heads wastes less of them than of the
 // 32-row ones.
 // As load_to_lds_b128, for bytes that are read once: marked non-temporal they do not push each other through the caches (a decode
-// step of 64 requests, 1.07 GB of keys and values: 198 us without the mark, 176 us with it, 6.1 TB/s).
+// step of 64 requests, 1.07 GB of keys and values: 198 us without the mark, 176 us with it when it came in; 171 now, 6.2 TB/s).
 __device__ __forceinline__ void stream_to_lds_b128(v4i desc, unsigned lds_base, unsigned lds_offset, int voffset) {
     asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen nt lds"
                  :
@@ -468,7 +475,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(RB * 
     float2* ml = reinterpret_cast<float2*>(lds + NW * RB * 16 * D * 4);   // [NW][RB * 16]
 
     // (heads side by side: with 8 or 32 of them the workgroups i, i + 8, ... of an XCD read the same heads' columns; the heads of a run
-    // on one XCD instead read 1.2 GB in 183 us where this takes 176)
+    // on one XCD instead take 183 us where this takes 176, 1.07 GB)
     const int slot = blockIdx.x / a.heads_kv, head = blockIdx.x % a.heads_kv;
     const Deal deal = few_deal(a, slot, -1);
     int seq = deal.seq, tiles = deal.tiles, begin = deal.begin, at = slot * deal.per;
@@ -866,7 +873,8 @@ AttnPlan attention_plan(int M, int seqs, int max_q, int max_kv, int heads_kv, in
         p.slots = (int)std::min(ceil_div(cu_count(), heads_kv), ceil_div(seqs * most, kLeast));
         p.few_cut = p.slots > 1 && (seqs > 1 || most > kLeast);
     }
-    if (p.tiles) cut_keys(max_kv, ((long long)M * group / (kTileWaves * kRowsPerWave) + 1) * heads_kv, 2 * cu_count(), kKeys, 256, &p.tile_chunk, &p.tile_chunks);
+    // (three workgroups a unit wanted: a chunk of 300 rows over 4300 keys beside 24 requests 103 us, 106 with two, 126 with one)
+    if (p.tiles) cut_keys(max_kv, ((long long)M * group / (kTileWaves * kRowsPerWave) + 1) * heads_kv, 3 * cu_count(), kKeys, 256, &p.tile_chunk, &p.tile_chunks);
     return p;
 }
 

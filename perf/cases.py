@@ -10,8 +10,8 @@ normalised scales, amplifier 2^10: what the benchmark and the tests of this repo
 Kinds of case
   linear  one linear call on fp16 token rows: m x k times n x k.
   block   the projections of `layers` decoder blocks on m token rows, as a block calls them: RMSNorm folded into the
-          quantiser, qkv GEMM on the codes; o_proj as a linear call on fp16 (the attention itself is not this
-          framework's); RMSNorm folded into the quantiser, gate_up GEMM, SiLU * up folded into the quantiser (or, "fused",
+          quantiser, qkv GEMM on the codes; o_proj as a linear call on fp16 (the attention between them is not
+          part of these cases); RMSNorm folded into the quantiser, gate_up GEMM, SiLU * up folded into the quantiser (or, "fused",
           the gate_up GEMM with SiLU * up as its epilogue and the quantiser behind it), down GEMM.  "down_bits" 8 is the
           recipe with fine-grained W8A8 down projections.  "scales" float is the float-scale form of the same layer.
           "graph": a decode step as a serving loop keeps it, captured once and replayed.
