@@ -389,6 +389,18 @@ def _workspace(query, sizes, device, workspace):
     return ws, nbytes
 
 
+def _zeros(shape, dtype, device, stream):
+    """A zero-filled tensor for a call on `stream` (None: the current one).  It is allocated and filled on that stream: a fill on
+    the current one would be queued inside the call, where no caller can order it before the call's kernels."""
+    torch = _torch()
+    if stream is None:
+        return torch.zeros(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.zeros(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream())  # (whoever gets it reads it there, most likely)
+    return t
+
+
 def _release_workspace(ws, workspace, stream) -> None:
     """A workspace this module allocated goes back to torch's allocator when the call returns, while the kernels may
     still be queued: tell the allocator which stream uses it, so the block is not handed out on another stream early."""
@@ -1186,7 +1198,7 @@ def is_attention(q, k, v, q_offsets, head_dim: int, max_q_len: int, max_kv_len: 
     if head_dim <= 0 or wq % head_dim or wk % head_dim:
         raise ValueError(f"q, k: {wq} and {wk} columns are no whole heads of {head_dim}")
     if out is None:
-        out = _torch().zeros((M, wq), dtype=_half_dtype, device=q.device)
+        out = _zeros((M, wq), _half_dtype, q.device, stream)
     ldq, ldo = _rows(q, M, wq, device, "q"), _rows(out, M, wq, device, "out")
     ldk, ldv = _rows(k, rows, wk, device, "k"), _rows(v, rows, wk, device, "v")
     _vector(q_offsets, _int32_dtype, seqs + 1, device, "q_offsets")

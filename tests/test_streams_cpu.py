@@ -1,0 +1,81 @@
+"""What a call on a stream of its own allocates and fills: on that stream, or nothing would order the fill before the call's kernels.
+The binding alone, with host tensors, a library that only notes its calls and streams that only have a number."""
+import contextlib
+
+import pytest
+import torch
+
+from paper_2405_14597_amd import binding
+
+
+class Stream:
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
+class Torch:
+    """torch with fills that note the stream they are queued on."""
+
+    def __init__(self, log):
+        self.log, self.queue = log, [Stream(0)]
+        self.cuda = self
+
+    def __getattr__(self, name):
+        return getattr(torch, name)
+
+    @contextlib.contextmanager
+    def stream(self, s):
+        self.queue.append(s)
+        yield
+        self.queue.pop()
+
+    def current_stream(self):
+        return self.queue[-1]
+
+    def zeros(self, shape, dtype, device):
+        self.log.append(("fill", self.queue[-1].cuda_stream))
+        return Tensor(torch.zeros(shape, dtype=dtype))
+
+
+class Tensor(torch.Tensor):
+    @staticmethod
+    def __new__(cls, t):
+        return torch.Tensor._make_subclass(cls, t)
+
+    def record_stream(self, s):
+        pass
+
+
+@pytest.fixture
+def log(monkeypatch):
+    got = []
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                if name.endswith("_bytes"):
+                    return 64
+                got.append(("kernels", args[-1]))
+                return 0
+            return call
+
+    fake = Torch(got)
+    monkeypatch.setattr(binding, "_torch", lambda: fake)
+    monkeypatch.setattr(binding, "load_library", lambda lib=Library(): lib)
+    monkeypatch.setattr(binding, "_current_raw_stream", lambda device: 0)
+    monkeypatch.setattr(binding, "_current_device", lambda: -1)
+    monkeypatch.setattr(binding, "_device_of", lambda t, name: -1)
+    monkeypatch.setattr(binding, "_require", lambda *a: None)
+    for name, dtype in (("_half_dtype", torch.float16), ("_int32_dtype", torch.int32), ("_int64_dtype", torch.int64), ("_float_dtype", torch.float32)):
+        monkeypatch.setattr(binding, name, dtype, raising=False)
+    return got
+
+
+@pytest.mark.parametrize("stream", [None, Stream(7)], ids=["current", "another"])
+def test_attention_fills_a_new_output_on_its_stream(log, stream):
+    half = lambda *s: torch.zeros(s, dtype=torch.float16)  # noqa: E731
+    out = binding.is_attention(half(3, 128), half(3, 128), half(3, 128), torch.zeros(2, dtype=torch.int32), 64, 3, 3, stream=stream,
+                               workspace=torch.zeros(64, dtype=torch.uint8))
+    assert out.shape == (3, 128)
+    on = 0 if stream is None else 7
+    assert log == [("fill", on), ("kernels", on)]
