@@ -834,14 +834,14 @@ def is_describe_grouped_prepacked(num_experts: int, M_total: int, N: int, K: int
     return buf.value.decode().split("\n")
 
 
-def _zero_workspace(query, sizes, device, workspace):
+def _zero_workspace(query, sizes, device, workspace, stream):
     """The prepacked GEMMs want their arrival counters zero: a fresh workspace is zero-filled."""
     if workspace is not None:
         return workspace, workspace.numel() * workspace.element_size()
     nbytes = query(*sizes)
     if nbytes == 0:
         return None, 0
-    return _torch().zeros((nbytes,), dtype=_torch().uint8, device=device), nbytes
+    return _zeros((nbytes,), _torch().uint8, device, stream), nbytes
 
 
 def is_gemm_w4a8_intscale_prepacked(xq, a_scale, packed: PackedWeights, chan_scale, alpha_log2: int, out=None,
@@ -863,7 +863,7 @@ def is_gemm_w4a8_intscale_prepacked(xq, a_scale, packed: PackedWeights, chan_sca
         acc_out = torch.empty((M, N), dtype=torch.int32, device=xq.device)
     if acc_out is not None:
         _require(acc_out, torch.int32, (M, N), "acc_out")
-    ws, ws_bytes = _zero_workspace(is_gemm_prepacked_workspace_bytes, (M, N, K, group), xq.device, workspace)
+    ws, ws_bytes = _zero_workspace(is_gemm_prepacked_workspace_bytes, (M, N, K, group), xq.device, workspace, stream)
     st = load_library().is_gemm_w4a8_intscale_prepacked(_p(xq), _p(a_scale), _p(packed.wpack), _p(packed.spack),
                                                        _p(chan_scale), M, N, K, group, alpha_log2, _p(out), _p(acc_out),
                                                        _p(ws), ws_bytes, _stream_handle(stream))
@@ -928,7 +928,7 @@ def is_gemm_w4a8_intscale_gate_up_silu_prepacked(xq, a_scale, gate_up: PackedGat
     if acc_out is not None:
         _require(acc_out, torch.int32, (M, 2 * inter), "acc_out")
     ws, ws_bytes = _zero_workspace(is_gemm_gate_up_silu_prepacked_workspace_bytes, (M, inter, K, packed.group), xq.device,
-                                   workspace)
+                                   workspace, stream)
     st = load_library().is_gemm_w4a8_intscale_gate_up_silu_prepacked(
         _p(xq), _p(a_scale), _p(packed.wpack), _p(packed.spack), _p(gate_up.chan_scale), M, inter, K, packed.group,
         alpha_log2, _p(out), _p(acc_out), _p(ws), ws_bytes, _stream_handle(stream))
@@ -950,7 +950,7 @@ def is_gemm_w4a8_floatscale_gate_up_silu_prepacked(xq, a_scale, gate_up: PackedG
         out = torch.empty((M, inter), dtype=torch.float16, device=xq.device)
     _require(out, torch.float16, (M, inter), "out")
     ws, ws_bytes = _zero_workspace(is_gemm_gate_up_silu_prepacked_workspace_bytes, (M, inter, K, packed.group), xq.device,
-                                   workspace)
+                                   workspace, stream)
     st = load_library().is_gemm_w4a8_floatscale_gate_up_silu_prepacked(
         _p(xq), _p(a_scale), _p(packed.wpack), _p(packed.spack), M, inter, K, packed.group, _p(out), _p(ws), ws_bytes,
         _stream_handle(stream))
@@ -1051,7 +1051,7 @@ def is_gemm_w4a8_floatscale_prepacked(xq, a_scale, packed: PackedWeights, out=No
     if out is None:
         out = torch.empty((M, N), dtype=torch.float16, device=xq.device)
     _require(out, torch.float16, (M, N), "out")
-    ws, ws_bytes = _zero_workspace(is_gemm_prepacked_workspace_bytes, (M, N, K, group), xq.device, workspace)
+    ws, ws_bytes = _zero_workspace(is_gemm_prepacked_workspace_bytes, (M, N, K, group), xq.device, workspace, stream)
     st = load_library().is_gemm_w4a8_floatscale_prepacked(_p(xq), _p(a_scale), _p(packed.wpack), _p(packed.spack), M, N,
                                                          K, group, _p(out), _p(ws), ws_bytes, _stream_handle(stream))
     _check("is_gemm_w4a8_floatscale_prepacked", st)
@@ -1077,7 +1077,7 @@ def is_linear_w4a8_intscale_prepacked(x, packed: PackedWeights, chan_scale, alph
         acc_out = torch.empty((M, N), dtype=torch.int32, device=x.device)
     if acc_out is not None:
         _require(acc_out, torch.int32, (M, N), "acc_out")
-    ws, ws_bytes = _zero_workspace(is_linear_prepacked_workspace_bytes, (M, N, K, group), x.device, workspace)
+    ws, ws_bytes = _zero_workspace(is_linear_prepacked_workspace_bytes, (M, N, K, group), x.device, workspace, stream)
     st = load_library().is_linear_w4a8_intscale_prepacked(_p(x), _p(packed.wpack), _p(packed.spack), _p(chan_scale), M, N,
                                                          K, group, alpha_log2, _p(out), _p(acc_out), _p(ws), ws_bytes,
                                                          _stream_handle(stream))
@@ -1096,7 +1096,7 @@ def is_linear_w4a8_floatscale_prepacked(x, packed: PackedWeights, out=None, work
     if out is None:
         out = torch.empty((M, N), dtype=torch.float16, device=x.device)
     _require(out, torch.float16, (M, N), "out")
-    ws, ws_bytes = _zero_workspace(is_linear_prepacked_workspace_bytes, (M, N, K, group), x.device, workspace)
+    ws, ws_bytes = _zero_workspace(is_linear_prepacked_workspace_bytes, (M, N, K, group), x.device, workspace, stream)
     st = load_library().is_linear_w4a8_floatscale_prepacked(_p(x), _p(packed.wpack), _p(packed.spack), M, N, K, group,
                                                            _p(out), _p(ws), ws_bytes, _stream_handle(stream))
     _check("is_linear_w4a8_floatscale_prepacked", st)

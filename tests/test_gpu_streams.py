@@ -32,3 +32,23 @@ def test_attention_with_an_output_of_its_own():
     torch.cuda.synchronize()
     assert torch.equal(now, want) and torch.equal(got, want)
     del keep
+
+
+def test_prepacked_gemm_with_a_workspace_of_its_own():
+    # K cut over workgroups, which meet by arrival counters in the workspace
+    M, N, K, G = 4, 64, 65536, 128
+    g = torch.Generator().manual_seed(5)
+    q = torch.randint(0, 256, (N, K // 2), dtype=torch.uint8, generator=g).to(DEV)
+    si = torch.randint(1, 1025, (N, K // G), dtype=torch.int32, generator=g).to(DEV)
+    xq = torch.randint(-127, 128, (M, K), dtype=torch.int8, generator=g).to(DEV)
+    sa, chan = (torch.rand(n, generator=g).to(DEV) * 1e-3 for n in (M, N))
+    packed = P.is_prepack_w4(q, si, G)
+    assert P.is_gemm_prepacked_workspace_bytes(M, N, K, G) > 0 and P.is_describe_prepacked(M, N, K, G)[0].startswith("gemm_decode_pk_kernel<")
+    want = P.is_gemm_w4a8_intscale_prepacked(xq, sa, packed, chan, 10, want_acc=True)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    keep = busy()
+    got = P.is_gemm_w4a8_intscale_prepacked(xq, sa, packed, chan, 10, want_acc=True, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    del keep

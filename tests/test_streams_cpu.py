@@ -79,3 +79,27 @@ def test_attention_fills_a_new_output_on_its_stream(log, stream):
     assert out.shape == (3, 128)
     on = 0 if stream is None else 7
     assert log == [("fill", on), ("kernels", on)]
+
+
+W = torch.zeros(8, dtype=torch.uint8)
+X, XQ, SA = torch.zeros((4, 128), dtype=torch.float16), torch.zeros((4, 128), dtype=torch.int8), torch.zeros(4)
+
+
+def packed(floats):
+    return binding.PackedWeights(W, W, 16, 128, 128, floats)
+
+
+@pytest.mark.parametrize("stream", [None, Stream(7)], ids=["current", "another"])
+@pytest.mark.parametrize("call", [
+    lambda s: binding.is_gemm_w4a8_intscale_prepacked(XQ, SA, packed(False), None, 10, stream=s),
+    lambda s: binding.is_gemm_w4a8_floatscale_prepacked(XQ, SA, packed(True), stream=s),
+    lambda s: binding.is_linear_w4a8_intscale_prepacked(X, packed(False), None, 10, stream=s),
+    lambda s: binding.is_linear_w4a8_floatscale_prepacked(X, packed(True), stream=s),
+    lambda s: binding.is_gemm_w4a8_intscale_gate_up_silu_prepacked(XQ, SA, binding.PackedGateUp(packed(False), None, 16), 10, stream=s),
+    lambda s: binding.is_gemm_w4a8_floatscale_gate_up_silu_prepacked(XQ, SA, binding.PackedGateUp(packed(True), None, 16), stream=s)],
+    ids=["gemm", "gemm_float", "linear", "linear_float", "gate_up", "gate_up_float"])
+def test_prepacked_calls_zero_a_new_workspace_on_their_stream(log, call, stream):
+    # (the kernels count on arrival counters of zero)
+    call(stream)
+    on = 0 if stream is None else 7
+    assert log == [("fill", on), ("kernels", on)]
