@@ -276,10 +276,11 @@ def _stream_handle(stream) -> int:
     if _current_raw_stream is None:
         torch = _torch()
         current = torch.cuda.current_stream()   # (initialises CUDA where nothing has yet)
-        _current_device = getattr(torch._C, "_cuda_getDevice", None)
-        _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        if _current_device is None or _current_raw_stream is None:
-            _current_device, _current_raw_stream = int, lambda _: int(torch.cuda.current_stream().cuda_stream)
+        device, raw = getattr(torch._C, "_cuda_getDevice", None), getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if device is None or raw is None:
+            device, raw = torch.cuda.current_device, lambda _: int(torch.cuda.current_stream().cuda_stream)
+        # (in this order: other threads go by the second)
+        _current_device, _current_raw_stream = device, raw
         return int(current.cuda_stream)
     return _current_raw_stream(_current_device())
 
