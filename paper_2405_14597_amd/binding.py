@@ -1117,7 +1117,8 @@ def _device_of(t, name) -> int:
     global _half_dtype, _int32_dtype, _int64_dtype, _float_dtype
     if _half_dtype is None:
         torch = _torch()
-        _half_dtype, _int32_dtype, _int64_dtype, _float_dtype = torch.float16, torch.int32, torch.int64, torch.float32
+        # (in this order: other threads go by the last)
+        _int32_dtype, _int64_dtype, _float_dtype, _half_dtype = torch.int32, torch.int64, torch.float32, torch.float16
     device = t.get_device()
     if device < 0 or device != (_current_device or _torch().cuda.current_device)():
         raise ValueError(f"{name}: expected a tensor on the current cuda device, got one on {t.device}")

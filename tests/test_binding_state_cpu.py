@@ -43,7 +43,7 @@ def fresh(request, monkeypatch):
         monkeypatch.setattr(binding, name, None)
 
 
-@pytest.mark.parametrize("fn", ["_stream_handle"])
+@pytest.mark.parametrize("fn", list(KEPT))
 def test_no_moment_with_a_part_of_it(fresh, fn):
     tested, rest = KEPT[fn][0], KEPT[fn][1:]
     seen = []
