@@ -172,7 +172,9 @@ __global__ __launch_bounds__(kLoraWaves* kWave) void lora_inner_kernel(LoraArgs 
 #pragma unroll
             for (int i = 0; i < RT; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) t[b][i][j] = mine[b] == e ? s[b][i][j] : t[b][i][j];
+                for (int j = 0; j < 4; ++j)
+                    // (past the rank by a choice, too: the zeros above times an infinity of x would be NaN)
+                    t[b][i][j] = mine[b] != e ? t[b][i][j] : i * 16 + quad * 4 + j < rank ? s[b][i][j] : 0.0f;
     }
 #pragma unroll
     for (int b = 0; b < CB; ++b)

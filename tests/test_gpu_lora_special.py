@@ -1,0 +1,36 @@
+"""is_lora_add where values are not ordinary: in the form by rows and in that by tiles (narrow and wide stores), which have to agree with
+the formula alike."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2405_14597_amd as P
+from oracle import block as B
+from test_gpu_lora import DEV, FORMS, check, make, on, want
+
+pytestmark = pytest.mark.gpu
+
+
+def add(c):
+    d = on(c)
+    return P.is_lora_add(d["x"], d["a"], d["b"], d["e"], d["base"], scales=d["scales"], ranks=d["ranks"])
+
+
+@FORMS
+def test_an_infinity_in_x_and_what_lies_past_the_rank(M, N, R):
+    # adapters of rank 0, 1, 5 and all of R; what a row of A past the rank makes of an infinity does not count
+    c = make(M, N, 72, R, 4, 17, "rows")
+    c["ranks"] = torch.tensor([0, 1, 5, R], dtype=torch.int32)
+    c["e"] = (torch.arange(M) % 5 - 1).int()
+    odd = torch.arange(M) % 3 == 1
+    c["a"][:, :, 7] = c["a"][:, :, 7].abs() + 0.1
+    c["b"] = c["b"].abs() + 0.01
+    ref = want(c)
+    c["x"][odd, 7] = float("inf")
+    got = add(c)
+    fine = (~odd | (c["e"] < 1)).numpy()      # (no adapter or one of rank 0: the base, whatever x is)
+    assert odd[torch.from_numpy(fine)].any()
+    check(got[torch.from_numpy(fine).to(DEV)], (ref[0][fine], ref[1][fine]), "rows that no infinity reaches")
+    nothing = (c["e"] < 1).to(DEV)
+    assert torch.equal(got[nothing], c["base"].to(DEV)[nothing])
+    assert (got[torch.from_numpy(~fine).to(DEV)] == float("inf")).all()
