@@ -77,9 +77,11 @@ def lora_add(x, a, b, row_adapter, base, scales, ranks):
         ae, be = np.asarray(a[e][:r], dtype=np.float64), np.asarray(b[e][:, :r], dtype=np.float64)
         t = ae @ x[m]
         out[m] += scales[e] * (be @ t)
-        # K products summed in fp32 (in any order), two fp16 terms of the inner product (2^-22 of the row's largest; 2^-24 and
-        # more below it end in fp16's smallest step), R products summed in fp32, a factor and a sum
-        inner = (k + 40) * F * (np.abs(ae) @ np.abs(x[m])) + 2.0 ** -21 * np.abs(t).max(initial=0.0)
+        # K products summed in fp32 (in any order), the inner product as two fp16 terms (the first to half a step or 2^-25 of a power of
+        # two at the row's largest, the second likewise of 2^27 times what is left), R products summed in fp32, a factor and a sum
+        size = np.abs(t)
+        most = size.max(initial=0.0)
+        inner = (k + 40) * F * (np.abs(ae) @ np.abs(x[m])) + H * H * size + np.minimum(H * size, 2.0 ** -35 * most) + 2.0 ** -51 * most
         outer = abs(scales[e]) * (np.abs(be) @ inner + (r + 8) * F * (np.abs(be) @ np.abs(t)))
         bound[m] = H * np.abs(out[m]) + outer + 2 * F * np.abs(out[m]) + TINY
     return out, bound

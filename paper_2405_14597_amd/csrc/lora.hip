@@ -196,9 +196,12 @@ __global__ __launch_bounds__(kLoraWaves* kWave) void lora_inner_kernel(LoraArgs 
 
 // out = base + scale t B^T: 32 rows x 32 columns a wave, 64 x 64 a workgroup.  First operand: rows of B (columns of out),
 // second: t.  Row i of operand tile j is column 16 (i / 4) + 4 j + i % 4, so that a lane's four results of the four tiles are 16
-// columns in a row.  t goes in as two fp16 terms (together 2^-22 of the row's largest) after a power of two of the row: rounded to
-// one it would add an error of the size of the output's own rounding, and a large t would overflow.  The terms are made once a
-// workgroup, for `steps` tiles of 64 columns, and lie in LDS as the instructions take them.
+// columns in a row.  t goes in as two fp16 terms, the row's largest brought to [0.5, 1) by a power of two: rounded to one it would add an
+// error of the size of the output's own rounding, and a large t would overflow.  The second term is what the first leaves, at most 2^-12,
+// times 2^27, with an accumulator of its own: so it stays a normal number, and a t[r] far below the row's largest keeps its bits (to 2^-22
+// of itself, 2^-11 at worst; without the factor all below 2^-25 of the largest was lost).  The terms are made once a workgroup, for `steps`
+// tiles of 64 columns, and lie in LDS as the instructions take them.
+constexpr float kLowUp = 0x1p27f;
 template <int RS>  // R in steps of 32
 __global__ __launch_bounds__(kLoraWaves* kWave) void lora_outer_kernel(LoraArgs a, int wide, int steps) {
     constexpr int CB = kOuterBlocks, kBlocks = kOuterRows / 16;
@@ -248,7 +251,7 @@ __global__ __launch_bounds__(kLoraWaves* kWave) void lora_outer_kernel(LoraArgs 
             for (int i = 0; i < 8; ++i) {
                 const float v = __builtin_amdgcn_ldexpf(t[s][i], up);
                 h[i] = (_Float16)v;
-                l[i] = fabsf(v) < INFINITY ? (_Float16)(v - (float)h[i]) : (_Float16)0.0f;
+                l[i] = fabsf(v) < INFINITY ? (_Float16)(kLowUp * (v - (float)h[i])) : (_Float16)0.0f;
             }
             hi[wave][s][lane] = h;
             lo[wave][s][lane] = l;
@@ -303,12 +306,14 @@ __global__ __launch_bounds__(kLoraWaves* kWave) void lora_outer_kernel(LoraArgs 
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int b = 0; b < CB; ++b) {
-                f4 s = f4{0.0f, 0.0f, 0.0f, 0.0f};
+                f4 s = f4{0.0f, 0.0f, 0.0f, 0.0f}, low = s;
 #pragma unroll
                 for (int st = 0; st < RS; ++st) {
                     s = __builtin_amdgcn_mfma_f32_16x16x32_f16(wv[j][st], hi[b0 + b][st][lane], s, 0, 0, 0);
-                    s = __builtin_amdgcn_mfma_f32_16x16x32_f16(wv[j][st], lo[b0 + b][st][lane], s, 0, 0, 0);
+                    low = __builtin_amdgcn_mfma_f32_16x16x32_f16(wv[j][st], lo[b0 + b][st][lane], low, 0, 0, 0);
                 }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] = fmaf(low[i], 1.0f / kLowUp, s[i]);
                 const float back = __builtin_amdgcn_ldexpf(scale, power[(b0 + b) * 16 + col]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum[b][j][i] = mine[b] == e ? back * s[i] : sum[b][j][i];

@@ -34,3 +34,22 @@ def test_an_infinity_in_x_and_what_lies_past_the_rank(M, N, R):
     nothing = (c["e"] < 1).to(DEV)
     assert torch.equal(got[nothing], c["base"].to(DEV)[nothing])
     assert (got[torch.from_numpy(~fine).to(DEV)] == float("inf")).all()
+
+
+@FORMS
+def test_inner_products_of_very_different_size(M, N, R):
+    # from r to r the inner products fall by 2^24 in all and B's columns grow by as much: every r counts alike
+    K = 4 * R
+    c = make(M, N, K, R, 3, 19, "rows")
+    c["ranks"][:] = torch.tensor([R, R - 3, R])
+    fall = torch.exp2(-12.0 * torch.arange(R) / (R - 1))
+    own = (torch.arange(K) // 4 == torch.arange(R)[:, None])
+    g = torch.Generator().manual_seed(21)
+    c["x"] = ((torch.rand((M, K), generator=g) + 0.5) * 64 * fall.repeat_interleave(4)).half()
+    c["a"] = ((torch.rand((3, R, K), generator=g) + 0.5) * own * fall[:, None]).half()
+    c["b"] = (torch.randn((3, N, R), generator=g) * 2.0 ** -12 / fall ** 2).half()
+    c["base"] *= 0.01
+    ref = want(c)
+    part = lambda e, lo, hi: c["b"][e, :, lo:hi].double() @ (c["a"][e, lo:hi].double() @ c["x"][0].double())  # noqa: E731
+    assert part(0, 0, 2).abs().mean() < 4 * part(0, R - 2, R).abs().mean() and part(0, R - 2, R).abs().mean() < 4 * part(0, 0, 2).abs().mean()
+    check(add(c), ref, "spread")
