@@ -194,6 +194,21 @@ __global__ __launch_bounds__(kLoraWaves* kWave) void lora_inner_kernel(LoraArgs 
     }
 }
 
+// One element of scale t B^T as it stands in the formula, for those that are not finite: of an infinity (of B's, of t's) a second term of
+// zero or of the other sign makes NaN, and a row with an infinite t[r] has no power of two that keeps its others from overflowing.
+__device__ __forceinline__ float plain_product(const LoraArgs& a, int row, int e, int n) {
+    const int rank = rank_of(a, e);
+    float y = 0.0f;
+#pragma unroll 1
+    for (int r = 0; r < rank; ++r) {
+        float t = 0.0f;
+#pragma unroll 1
+        for (int slab = 0; slab < a.slabs; ++slab) t += a.inner[((size_t)slab * a.M + row) * a.R + r];
+        y = fmaf(__half2float(a.b[((size_t)e * a.N + n) * a.R + r]), t, y);
+    }
+    return a.scales ? a.scales[e] * y : y;
+}
+
 // out = base + scale t B^T: 32 rows x 32 columns a wave, 64 x 64 a workgroup.  First operand: rows of B (columns of out),
 // second: t.  Row i of operand tile j is column 16 (i / 4) + 4 j + i % 4, so that a lane's four results of the four tiles are 16
 // columns in a row.  t goes in as two fp16 terms, the row's largest brought to [0.5, 1) by a power of two: rounded to one it would add an
@@ -203,7 +218,7 @@ __global__ __launch_bounds__(kLoraWaves* kWave) void lora_inner_kernel(LoraArgs 
 // tiles of 64 columns, and lie in LDS as the instructions take them.
 constexpr float kLowUp = 0x1p27f;
 template <int RS>  // R in steps of 32
-__global__ __launch_bounds__(kLoraWaves* kWave) void lora_outer_kernel(LoraArgs a, int wide, int steps) {
+__global__ __launch_bounds__(kLoraWaves* kWave) __attribute__((amdgpu_waves_per_eu(RS <= 2 ? 4 : 2))) void lora_outer_kernel(LoraArgs a, int wide, int steps) {
     constexpr int CB = kOuterBlocks, kBlocks = kOuterRows / 16;
     __shared__ h8 hi[kBlocks][RS][kWave], lo[kBlocks][RS][kWave];
     __shared__ int power[kOuterRows];
@@ -217,7 +232,7 @@ __global__ __launch_bounds__(kLoraWaves* kWave) void lora_outer_kernel(LoraArgs 
         all[b] = __ballot(mine[b] >= 0);
     }
     // ---- block `wave` of t
-    static_assert(kBlocks == kLoraWaves, "a wave makes the terms of one block");
+    static_assert(kBlocks == kLoraWaves && CB == 2, "a wave makes the terms of one block and has the results of two");
     {
         const int row = blockIdx.y * kOuterRows + wave * 16 + col;
         const bool has = own_adapter(a, row) >= 0;
@@ -314,9 +329,9 @@ __global__ __launch_bounds__(kLoraWaves* kWave) void lora_outer_kernel(LoraArgs 
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[i] = fmaf(low[i], 1.0f / kLowUp, s[i]);
-                const float back = __builtin_amdgcn_ldexpf(scale, power[(b0 + b) * 16 + col]);
+                const int up = power[(b0 + b) * 16 + col];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[b][j][i] = mine[b] == e ? back * s[i] : sum[b][j][i];
+                for (int i = 0; i < 4; ++i) sum[b][j][i] = mine[b] == e ? scale * __builtin_amdgcn_ldexpf(s[i], up) : sum[b][j][i];
             }
     };
     for (int step = 0; step < steps && first_column(step) < a.N; ++step) {
@@ -330,6 +345,19 @@ __global__ __launch_bounds__(kLoraWaves* kWave) void lora_outer_kernel(LoraArgs 
             h8 wv[2][RS];
             load_b(wv, adapter_at(k), step);
             add(wv, adapter_at(k), rank_at(k), scale_at(k));
+        }
+        unsigned odd = 0;  // bit 8 b + i: result i of block b is not finite
+#pragma unroll
+        for (int i = 0; i < 8 * CB; ++i) odd |= fabsf(sum[i / 8][i % 8 / 4][i % 4]) < INFINITY ? 0u : 1u << i;
+        if (__builtin_expect(__any(odd != 0), 0)) {
+#pragma unroll 1
+            for (; odd != 0; odd &= odd - 1) {
+                const int at = __builtin_ctz(odd), b = at / 8;
+                const int e = b == 0 ? mine[0] : mine[1], column = n + at % 8;
+                const float y = column < a.N ? plain_product(a, blockIdx.y * kOuterRows + (b0 + b) * 16 + col, e, column) : 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8 * CB; ++i) sum[i / 8][i % 8 / 4][i % 4] = i == at ? y : sum[i / 8][i % 8 / 4][i % 4];
+            }
         }
 #pragma unroll
         for (int b = 0; b < CB; ++b) {
