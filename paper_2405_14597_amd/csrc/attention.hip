@@ -37,8 +37,17 @@ constexpr int kRowsPerWave = 32; // packed rows of a wave
 // probabilities are larger than 1, at most 2^8, which fp16 holds as exactly as those below 1, and the accumulators need no
 // rescaling.
 constexpr float kLazyMax = 8.0f;
+// A maximum past this (in powers of two) is subtracted from the scores by itself, before anything is added: the fused multiply-add with
+// the maximum, which is rounded, would leave what that rounding took (at 2^28 some powers of two, and the sum overflows or vanishes).
+constexpr float kFarMax = 4096.0f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// x * y, rounded before anything else is done with it.
+__device__ __forceinline__ float rounded_product(float x, float y) {
+    float p = x * y;
+    asm volatile("" : "+v"(p));
+    return p;
+}
 
 // Maximum (sum) of a value and of the one in the other half of the wave (lane ^ 32).
 __device__ __forceinline__ float halves_max(float v) {
@@ -236,6 +245,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2))) 
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[b][i] = 0.0f;
     float top = -INFINITY, sum = 0.0f;  // running maximum of scale * q.k (powers of two), sum over this lane's half of the keys
+    bool far = false;                   // a row's maximum is past kFarMax
     const float factor = a.scale * 1.44269504088896340736f;
 
     const int t0 = c0 / kKeys, t1 = (min(c0 + a.tile_chunk, wg_most) + kKeys - 1) / kKeys;
@@ -303,7 +313,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2))) 
         float most = sc[0][0];
 #pragma unroll
         for (int i = 1; i < 32; ++i) most = fmaxf(most, sc[i / 16][i % 16]);
-        most = halves_max(most) * factor;
+        most = rounded_product(halves_max(most), factor);
         if (__any(most > top + kLazyMax)) {  // (the first tile too: top is -inf)
             const float now = fmaxf(top, most);
             const float shrink = now == -INFINITY ? 1.0f : exp2_fast(top - now);
@@ -313,12 +323,18 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2))) 
                 for (int i = 0; i < 16; ++i) o[b][i] *= shrink;
             sum *= shrink;
             top = now;
+            far = __any(fabsf(top) > kFarMax && top != -INFINITY);
         }
-        const float less = top == -INFINITY ? 0.0f : top;
+        float times = factor, less = top == -INFINITY ? 0.0f : top;
+        if (far) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) sc[i / 16][i % 16] = rounded_product(sc[i / 16][i % 16], factor) - less;
+            times = 1.0f, less = 0.0f;
+        }
         h8 pr[4];
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
-            const float p0 = exp2_fast(fmaf(sc[i / 16][i % 16], factor, -less)), p1 = exp2_fast(fmaf(sc[i / 16][i % 16 + 1], factor, -less));
+            const float p0 = exp2_fast(fmaf(sc[i / 16][i % 16], times, -less)), p1 = exp2_fast(fmaf(sc[i / 16][i % 16 + 1], times, -less));
             sum += p0 + p1;
             // (to the nearest, half a step of 2^-11 each: towards zero would leave every output too small)
             pr[i / 8][i % 8] = (_Float16)p0;
@@ -528,9 +544,10 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(RB * 
 
     v4f o[RB][kBlocks];
     float top[RB], sum[RB];
+    bool far[RB];
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-        top[b] = -INFINITY, sum[b] = 0.0f;
+        top[b] = -INFINITY, sum[b] = 0.0f, far[b] = false;
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) o[b][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     }
@@ -575,7 +592,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(RB * 
                 for (int i = 0; i < 8; ++i) x[i] = 16 * (i / 4) + i % 4 < seen ? x[i] : -INFINITY;
             }
             float most = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-            most = quads_max(most) * factor;
+            most = rounded_product(quads_max(most), factor);
             if (__any(most > top[b] + kLazyMax)) {
                 const float now = fmaxf(top[b], most);
                 const float shrink = now == -INFINITY ? 1.0f : exp2_fast(top[b] - now);
@@ -583,11 +600,17 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(RB * 
                 for (int i = 0; i < kBlocks; ++i) o[b][i] *= shrink;
                 sum[b] *= shrink;
                 top[b] = now;
+                far[b] = __any(fabsf(now) > kFarMax && now != -INFINITY);
             }
-            const float less = top[b] == -INFINITY ? 0.0f : top[b];
+            float times = factor, less = top[b] == -INFINITY ? 0.0f : top[b];
+            if (far[b]) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = rounded_product(x[i], factor) - less;
+                times = 1.0f, less = 0.0f;
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float p = exp2_fast(fmaf(x[i], factor, -less));
+                const float p = exp2_fast(fmaf(x[i], times, -less));
                 sum[b] += p;
                 pr[b][i] = (_Float16)p;
             }
