@@ -35,10 +35,11 @@ def attention(q, k, v, q_offsets, kv_starts, kv_lens, head_dim, scale, causal, u
                 out[at] = p @ values
                 # Each score: d products summed in fp32, scaled, an exponent of powers of two (its argument and the exponential a few
                 # steps): an error of e in a score is a factor 1 +- e, in the sum below the line as well.  Each probability is
-                # rounded to fp16 for the product with v, the sums run over `seen` terms in fp32.
+                # rounded to fp16 for the product with v, times 2^7 of the largest at least (below fp16's normal numbers half a
+                # step is 2^-25, 2^-32 of the largest).  The sums are fp32, a matrix instruction's 16 keys or a tile's 32 and more at a time.
                 e = scale * (d + 4) * F * (np.abs(keys) @ np.abs(x)).max() + 8 * F * (np.abs(z).max() + 4)
                 spread = p @ np.abs(values)
-                bound[at] = H * np.abs(out[at]) + spread * (H + 2 * e + 2 * (seen + 16) * F) + seen * TINY * np.abs(values).max() + TINY
+                bound[at] = H * np.abs(out[at]) + spread * (H + 2 * e + 2 * (seen / 16 + 64) * F) + 2.0 ** -32 * p.max() * np.abs(values).sum(0) + TINY
     return out, bound
 
 

@@ -33,10 +33,11 @@ typedef __attribute__((address_space(3))) unsigned char* LdsPtr;
 
 constexpr int kKeys = 64;        // keys of a tile
 constexpr int kRowsPerWave = 32; // packed rows of a wave
-// A row's running maximum is raised only when it would grow by more than this (in powers of two): until then the
-// probabilities are larger than 1, at most 2^8, which fp16 holds as exactly as those below 1, and the accumulators need no
-// rescaling.
-constexpr float kLazyMax = 8.0f;
+// A row's running maximum is raised only when it would grow by more than kLazyMax (in powers of two): until then the accumulators need
+// no rescaling.  The probabilities, fp16 for their product with V, are held times 2^kUp, the largest so far between 2^7 and 2^15: below
+// fp16's normal numbers half a step is then 2^-32 of it.  In a long tail beside one dominant key each key may be 2^-20 of that and less
+// (without the factor a tail of 131072 equal keys with 2 % of the weight came out 7 % off).  The factor is in the sum as well.
+constexpr float kLazyMax = 8.0f, kUp = 7.0f;
 // A maximum past this (in powers of two) is subtracted from the scores by itself, before anything is added: the fused multiply-add with
 // the maximum, which is rounded, would leave what that rounding took (at 2^28 some powers of two, and the sum overflows or vanishes).
 constexpr float kFarMax = 4096.0f;
@@ -245,6 +246,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2))) 
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[b][i] = 0.0f;
     float top = -INFINITY, sum = 0.0f;  // running maximum of scale * q.k (powers of two), sum over this lane's half of the keys
+    float less = 0.0f;                  // what the exponents are brought down by
     bool far = false;                   // a row's maximum is past kFarMax
     const float factor = a.scale * 1.44269504088896340736f;
 
@@ -324,22 +326,25 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2))) 
             sum *= shrink;
             top = now;
             far = __any(fabsf(top) > kFarMax && top != -INFINITY);
+            less = top == -INFINITY ? 0.0f : far ? -kUp : top - kUp;
         }
-        float times = factor, less = top == -INFINITY ? 0.0f : top;
+        float times = factor;
         if (far) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) sc[i / 16][i % 16] = rounded_product(sc[i / 16][i % 16], factor) - less;
-            times = 1.0f, less = 0.0f;
+            for (int i = 0; i < 32; ++i) sc[i / 16][i % 16] = rounded_product(sc[i / 16][i % 16], factor) - (top == -INFINITY ? 0.0f : top);
+            times = 1.0f;
         }
         h8 pr[4];
+        float part = 0.0f;  // (a sum of the tile's own: next to the running one the terms of a long tail would lose their bits one by one)
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
             const float p0 = exp2_fast(fmaf(sc[i / 16][i % 16], times, -less)), p1 = exp2_fast(fmaf(sc[i / 16][i % 16 + 1], times, -less));
-            sum += p0 + p1;
+            part += p0 + p1;
             // (to the nearest, half a step of 2^-11 each: towards zero would leave every output too small)
             pr[i / 8][i % 8] = (_Float16)p0;
             pr[i / 8][i % 8 + 1] = (_Float16)p1;
         }
+        sum += part;
         // V^T's operand: lane's column 32 b + (lane & 31), keys 16 s + 4 half + 0..3 and those 8 further on, as the probabilities lie
         const int vr = 4 * half + (lane & 15) / 4, vc = (lane >> 4 & 1) * 32 + (lane & 3) * 8;  // row, byte column
         auto values = [&](int step, int b) {
@@ -602,18 +607,19 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(RB * 
                 top[b] = now;
                 far[b] = __any(fabsf(now) > kFarMax && now != -INFINITY);
             }
-            float times = factor, less = top[b] == -INFINITY ? 0.0f : top[b];
+            float times = factor, less = top[b] == -INFINITY ? 0.0f : top[b] - kUp, part = 0.0f;
             if (far[b]) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = rounded_product(x[i], factor) - less;
-                times = 1.0f, less = 0.0f;
+                for (int i = 0; i < 8; ++i) x[i] = rounded_product(x[i], factor) - top[b];
+                times = 1.0f, less = -kUp;
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float p = exp2_fast(fmaf(x[i], times, -less));
-                sum[b] += p;
+                part += p;
                 pr[b][i] = (_Float16)p;
             }
+            sum[b] += part;
         }
         if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");

@@ -3,13 +3,20 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_attention import DEV, check, make, oracle, run
+import paper_2405_14597_amd as P
+from oracle import block as B
+from test_gpu_attention import DEV, check, make, run
 
 pytestmark = pytest.mark.gpu
 SEQS = pytest.mark.parametrize("seqs", [[(1, 700), (1, 40)], [(100, 100), (70, 200)], [(70, 6000)], [(3, 20000)]],
                                ids=["singles", "prompts", "chunk", "far"])
 HEADS = pytest.mark.parametrize("hq,hk,d", [(4, 2, 128), (8, 2, 64), (20, 1, 64)])
 H = 2.0 ** -11
+
+
+def oracle(c, causal, scale=None, **kw):
+    return B.attention(c["q"].numpy(), c["k"].numpy(), c["v"].numpy(), c["off"], c["starts"], c["lens"], c["d"],
+                       float(np.float32(c["d"] ** -0.5 if scale is None else scale)), causal, np.full(tuple(c["q"].shape), 7.0), **kw)
 
 
 @SEQS
@@ -37,3 +44,27 @@ def test_finite_scores_of_any_size(seqs, hq, hk, d):
                     want, size = (np.repeat(x.mean(0).reshape(hk, 1, d), hq // hk, 1).reshape(-1) for x in (v, np.abs(v)))
                     # (half a step of fp16 in the probabilities, which the sum below the line does not have, and half a step of the output)
                     assert (np.abs(got[q0 + i] - want) <= 1.01 * H * (np.abs(want) + size) + 2.0 ** -24).all(), (sign, scale, i)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("mass", [0.98, 0.92, 0.5])
+@pytest.mark.parametrize("form", ["row_tiles", "few_rows"])
+def test_a_long_tail_beside_a_dominant_key(form, mass, d):
+    # the first key takes most of the weight and has next to no value: what comes out is the tail's, all alike and 2^-20 or less of it
+    # each.  Enough rows that a workgroup walks all keys; every sequence over the same ones, and a few rows compared.
+    heads, keys, seqs = 8, 131072, 32
+    rows = 6400 // seqs if form == "row_tiles" else 1
+    g = torch.Generator(device=DEV).manual_seed(73)
+    normal = lambda n: torch.randn((n, heads * d), generator=g, device=DEV)  # noqa: E731
+    q, k, v = torch.zeros_like(normal(seqs * rows)).half(), normal(keys).half(), (normal(keys) * 0.3 + 1.0).half()
+    scale = d ** -0.5
+    q[:, ::d], k[:, ::d] = 4.0, 0.0
+    k[0, ::d], v[0] = float(np.log(mass / (1.0 - mass) * keys)) / (4.0 * scale), 0.01
+    whole = lambda x, t: torch.tensor(x, dtype=t, device=DEV)  # noqa: E731
+    got = P.is_attention(q, k, v, whole([i * rows for i in range(seqs + 1)], torch.int32), d, rows, keys, causal=False,
+                         kv_starts=whole([0] * seqs, torch.int64), kv_lens=whole([keys] * seqs, torch.int32))
+    at = [0, seqs * rows // 2, seqs * rows - 1]
+    head = slice(3 * d, 4 * d)   # (one head of the eight)
+    ref = B.attention(q[at, head].cpu().numpy(), k[:, head].cpu().numpy(), v[:, head].cpu().numpy(), [0, 3], [0], [keys], d,
+                      float(np.float32(scale)), False, np.zeros((3, d)))
+    check(got[at, head], ref, "tail")
