@@ -435,7 +435,8 @@ int is_qk_norm_rope(const void* q, int64_t ldq, const void* k, int64_t ldk, cons
  *   a row before the first key) is zero.
  * Scores, softmax statistics and sums in single precision; the probabilities are rounded to fp16 for their product with v, after a
  * factor of 2^7 over the largest so far (a key of less than 2^-21 of the largest probability counts to 2^-32 of that).  What
- * a row does not see does not reach it, whatever it holds (infinities and NaN among it).
+ * a row does not see does not reach it, whatever it holds (infinities and NaN among it); an infinity among the values that it sees makes
+ * its column infinite however small the key's probability (NaN beside one of the other sign, a NaN, or under a score of -inf).
  *   q, out       fp16 [M] rows of heads_q heads;  k, v  fp16 [kv_rows] rows of heads_kv heads
  *   q_offsets    int32 [num_seqs + 1], non-decreasing: rows [q_offsets[s], q_offsets[s+1]) of q and out are sequence s's.  Rows of
  *                out that belong to no sequence stay as they are.

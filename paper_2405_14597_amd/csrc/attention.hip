@@ -140,15 +140,6 @@ __device__ __forceinline__ float quads_sum(float v) {
     return halves_sum(__uint_as_float(s[0]) + __uint_as_float(s[1]));
 }
 
-// Whether an infinity or a NaN is among eight fp16 values in LDS.
-__device__ __forceinline__ bool has_odd_values(LdsPtr p) {
-    const v4i w = *(const __attribute__((address_space(3))) v4i*)p;
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) odd = odd || (w[i] & 0x7C00) == 0x7C00 || (w[i] & 0x7C000000) == 0x7C000000;
-    return odd;
-}
-
 // Sets the infinities and NaN among eight fp16 values in LDS to zero; whether there were any.
 __device__ __forceinline__ bool take_out_odd_values(LdsPtr p) {
     v4i w = *(const __attribute__((address_space(3))) v4i*)p;
@@ -162,6 +153,38 @@ __device__ __forceinline__ bool take_out_odd_values(LdsPtr p) {
     if (odd) *(__attribute__((address_space(3))) v4i*)p = w;
     return odd;
 }
+
+// Infinities and NaN among the values: a row's column that sees one is the sum of those it sees, however small their probabilities are (a
+// product with one that is rounded to zero, or a factor that vanishes later, would make NaN of an infinity).  The matrix instructions
+// leave such columns not finite, or the values were taken out of a tile that not every row sees; either is found once at the end of a
+// wave's keys, and the values are looked up then.
+__device__ __forceinline__ bool is_odd(float x) { return !(fabsf(x) < INFINITY); }
+// f * x, an infinity or a NaN as it is.
+__device__ __forceinline__ float times_unless_odd(float f, float x) { return is_odd(x) ? x : f * x; }
+
+// Keys `key` to `end` of a wave that looks such values up: each(key) for the keys of a tile that has one in the head's columns.
+template <int D, class Each>
+__device__ __forceinline__ void odd_tile(const __half* v_head, long long ldv, int key, int end, Each each) {
+    bool odd = false;
+#pragma unroll 1
+    for (int i = threadIdx.x & (kWave - 1); i < (end - key) * (D / 8); i += kWave) {
+        const v4i w = *reinterpret_cast<const v4i*>(v_head + (size_t)(key + i / (D / 8)) * ldv + i % (D / 8) * 8);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) odd = odd || (w[j] & 0x7C00) == 0x7C00 || (w[j] & 0x7C000000) == 0x7C000000;
+    }
+    if (!__any(odd)) return;
+#pragma unroll 1
+    for (; key < end; ++key) each(key);
+}
+// What such a value x of a key that the row sees comes to: itself, or the formula's 0 * x where the score is -inf.
+template <int D>
+__device__ __forceinline__ bool score_is_gone(const __half* q_row, const __half* k_row) {
+    float score = 0.0f;
+#pragma unroll 1
+    for (int i = 0; i < D; ++i) score = fmaf(__half2float(q_row[i]), __half2float(k_row[i]), score);
+    return !(score > -INFINITY);
+}
+__device__ __forceinline__ float odd_value(float x, bool gone) { return !is_odd(x) ? 0.0f : gone ? NAN : x; }
 
 // Where 16-byte chunk c of row r of a tile lies in LDS (in chunks from the row's start): rows are a power of two of bytes
 // apart, so without it the rows that one read touches would meet in the same banks.
@@ -248,6 +271,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2))) 
     float top = -INFINITY, sum = 0.0f;  // running maximum of scale * q.k (powers of two), sum over this lane's half of the keys
     float less = 0.0f;                  // what the exponents are brought down by
     bool far = false;                   // a row's maximum is past kFarMax
+    bool taken_out = false;             // infinities or NaN were taken out of a tile
     const float factor = a.scale * 1.44269504088896340736f;
 
     const int t0 = c0 / kKeys, t1 = (min(c0 + a.tile_chunk, wg_most) + kKeys - 1) / kKeys;
@@ -270,8 +294,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2))) 
         const LdsPtr kt = lds_p + buf * 2 * kTileBytes, vt = kt + kTileBytes;
         // Keys that some rows see and others do not: a product with a probability of zero still turns an infinity or a NaN among
         // their values into a NaN.  Such a tile is looked through first, and those values are taken out; the rows that see them get
-        // them below.
-        bool odd_values = false;
+        // them at the end.
         if (min((t + 1) * kKeys, s.kvlen) > wg_least) {
             bool odd = false;
 #pragma unroll
@@ -280,7 +303,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2))) 
             if (lane == 0) found[(t & 1) * NW + wave] = any_odd;
             __syncthreads();
 #pragma unroll
-            for (int w = 0; w < NW; ++w) odd_values = odd_values || found[(t & 1) * NW + w];
+            for (int w = 0; w < NW; ++w) taken_out = taken_out || found[(t & 1) * NW + w];
         }
         if (t * kKeys >= w_most) continue;  // (wave-uniform: no row of this wave sees the tile)
 
@@ -357,24 +380,30 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(2))) 
         for (int step = 0; step < 4; ++step)
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(values(step, b), pr[step], o[b], 0, 0, 0);
-        if (odd_values) {  // what was taken out, to the rows that see it (a probability is positive: times it, it stays what it is)
-#pragma unroll 1
-            for (int key = t * kKeys; key < min((t + 1) * kKeys, s.kvlen); ++key) {
-                const __half* src = v_head + (size_t)key * a.ldv + 4 * half;
-#pragma unroll
-                for (int i = 0; i < 16 * kBlocks; i += 4) {
-                    const h4 v = *reinterpret_cast<const h4*>(src + 2 * i);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float x = (float)v[j];
-                        if (key < lim && !(fabsf(x) < INFINITY)) o[i / 16][i % 16 + j] += x;
-                    }
-                }
-            }
-        }
     }
 
     sum = halves_sum(sum);
+    float none = 0.0f;  // 0, or NaN
+#pragma unroll
+    for (int i = 0; i < 16 * kBlocks; ++i) none = fmaf(0.0f, o[i / 16][i % 16], none);
+    if (__builtin_expect(__any((taken_out || is_odd(none)) && mine && !is_odd(sum)), 0)) {
+        const __half* q_row = a.q + (size_t)qrow * a.ldq + (size_t)qhead * D;
+#pragma unroll
+        for (int i = 0; i < 16 * kBlocks; ++i) o[i / 16][i % 16] = is_odd(o[i / 16][i % 16]) ? 0.0f : o[i / 16][i % 16];
+#pragma unroll 1
+        for (int t = t0; t < t1 && t * kKeys < w_most; ++t)
+            odd_tile<D>(v_head, a.ldv, t * kKeys, min((t + 1) * kKeys, w_most), [&](int key) {
+                if (key >= lim) return;
+                const bool gone = score_is_gone<D>(q_row, k_head + (size_t)key * a.ldk);
+                const __half* src = v_head + (size_t)key * a.ldv + 4 * half;
+#pragma unroll
+                for (int i = 0; i < 16 * kBlocks; i += 4) {  // columns as below
+                    const h4 v = *reinterpret_cast<const h4*>(src + 2 * i);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[i / 16][i % 16 + j] += odd_value((float)v[j], gone);
+                }
+            });
+    }
     if (s.kvlen <= a.tile_chunk) {
         // a row that sees no key is zero; one whose scores are all -inf (or that saw a NaN) is NaN, as the formula's 0 / 0
         const float inv = 1.0f / sum;
@@ -549,7 +578,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(RB * 
 
     v4f o[RB][kBlocks];
     float top[RB], sum[RB];
-    bool far[RB];
+    bool far[RB], taken_out = false;
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
         top[b] = -INFINITY, sum[b] = 0.0f, far[b] = false;
@@ -623,11 +652,11 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(RB * 
         }
         if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        bool odd = false;  // (keys that only some rows see, as in the kernel above)
-        if (min((t + 1) * kFewKeys, s.kvlen) > least) {
+        if (min((t + 1) * kFewKeys, s.kvlen) > least) {  // (keys that only some rows see, as in the kernel above)
+            bool odd = false;
 #pragma unroll
-            for (int i = 0; i < kTileBytes; i += 1024) odd = odd || has_odd_values(vt + i + lane * 16);
-            odd = __any(odd);
+            for (int i = 0; i < kTileBytes; i += 1024) odd = take_out_odd_values(vt + i + lane * 16) || odd;
+            taken_out = taken_out || __any(odd);
         }
         auto values = [&](int i) {  // V^T: column 16 i + (lane & 15), keys 4 quad + 0..3 and those 16 further on
             const int r = 4 * quad + (col >> 2), c = 2 * i + (col >> 1 & 1);
@@ -635,44 +664,54 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(RB * 
             const h4 y = lds_h4_turned(vt + (r + 16) * kRowBytes + few_v_chunk<D>(r + 16, c) * 16 + (col & 1) * 8);
             return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
         };
-        if (!odd) {
 #pragma unroll
-            for (int i = 0; i < kBlocks; ++i) {
-                const h8 v = values(i);
+        for (int i = 0; i < kBlocks; ++i) {
+            const h8 v = values(i);
 #pragma unroll
-                for (int b = 0; b < RB; ++b) o[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pr[b], o[b][i], 0, 0, 0);
-            }
-        } else {
-#pragma unroll 1
-            for (int key = 0; key < kFewKeys; ++key) {
-                const int e = (key / 16) * 4 + key % 4;
-                const bool here = (key / 4 & 3) == quad;
-#pragma unroll
-                for (int i = 0; i < kBlocks; ++i) {
-                    h8 v = values(i);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = j == e && here ? v[j] : (_Float16)0.0f;
-#pragma unroll
-                    for (int b = 0; b < RB; ++b) {
-                        h8 pk;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) pk[j] = j == e && here ? pr[b][j] : (_Float16)0.0f;
-                        const v4f one = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pk, v4f{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) o[b][i][j] = t * kFewKeys + key < lim[b] ? o[b][i][j] + one[j] : o[b][i][j];
-                    }
-                }
-            }
+            for (int b = 0; b < RB; ++b) o[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pr[b], o[b][i], 0, 0, 0);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (more) fetch(v_head, a.ldv, t + NW, v_off, kt_base + kTileBytes);
+    }
+
+    bool odd = false;  // infinities and NaN among the values, as in the kernel above
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+        sum[b] = quads_sum(sum[b]);
+        float none = 0.0f;  // 0, or NaN
+#pragma unroll
+        for (int i = 0; i < 4 * kBlocks; ++i) none = fmaf(0.0f, o[b][i / 4][i % 4], none);
+        odd = odd || ((taken_out || is_odd(none)) && lim[b] > 0 && !is_odd(sum[b]));
+    }
+    if (__builtin_expect(__any(odd), 0)) {
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4 * kBlocks; ++i) o[b][i / 4][i % 4] = is_odd(o[b][i / 4][i % 4]) ? 0.0f : o[b][i / 4][i % 4];
+#pragma unroll 1
+        for (t = t0 + wave; t < t1; t += NW)
+            odd_tile<D>(v_head, a.ldv, t * kFewKeys, min((t + 1) * kFewKeys, s.kvlen), [&](int key) {
+                const __half* src = v_head + (size_t)key * a.ldv + 4 * quad;
+#pragma unroll
+                for (int b = 0; b < RB; ++b) {
+                    const int p = b * 16 + col, row = p / a.group;
+                    if (key >= lim[b]) continue;
+                    const bool gone = score_is_gone<D>(a.q + (size_t)(s.q0 + row) * a.ldq + (size_t)(head * a.group + p - row * a.group) * D,
+                                                       k_head + (size_t)key * a.ldk);
+#pragma unroll
+                    for (int i = 0; i < kBlocks; ++i) {
+                        const h4 v = *reinterpret_cast<const h4*>(src + 16 * i);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) o[b][i][j] += odd_value((float)v[j], gone);
+                    }
+                }
+            });
     }
 
     // ---- the waves' results: lane's row 16 b + col, columns 16 i + 4 quad + 0..3
     __syncthreads();
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-        sum[b] = quads_sum(sum[b]);
         const int r = b * 16 + col;
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i)
@@ -697,6 +736,16 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(RB * 
             const float f = exp2_fast(m.x - less);
             total = fmaf(m.y, f, total);
             acc += f * *reinterpret_cast<const v4f*>(part + (size_t)(w * RB * 16 + r) * D + ((c + 4 * (r & 15)) & (D - 1)));
+        }
+        if (__builtin_expect(is_odd(acc[0] + acc[1] + acc[2] + acc[3]), 0)) {  // (a factor may have vanished)
+            acc = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+            for (int w = 0; w < NW; ++w) {
+                const float f = exp2_fast(ml[w * RB * 16 + r].x - less);
+                const v4f v = *reinterpret_cast<const v4f*>(part + (size_t)(w * RB * 16 + r) * D + ((c + 4 * (r & 15)) & (D - 1)));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[j] += times_unless_odd(f, v[j]);
+            }
         }
         if (whole) {
             const int row = r / a.group, seen = a.causal ? row + s.kvlen - s.qlen + 1 : s.kvlen;
@@ -747,14 +796,16 @@ __global__ __launch_bounds__(256) void attention_few_join_kernel(AttnArgs a) {
             for (int j = 0; j < kAtOnce; ++j) now = fmaxf(now, m[j].x);
             const float less = now == -INFINITY ? 0.0f : now, shrink = exp2_fast(top - less);
             sum *= shrink;
-            acc *= shrink;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] = times_unless_odd(shrink, acc[e]);
             top = now;
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j)
                 if (p0 + j <= last) {
                     const float f = exp2_fast(m[j].x - less);
                     sum = fmaf(m[j].y, f, sum);
-                    acc += f * v[j];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[e] += times_unless_odd(f, v[j][e]);
                 }
         }
         const int row = r / a.group, seen = a.causal ? row + s.kvlen - s.qlen + 1 : s.kvlen;
@@ -807,7 +858,7 @@ __global__ __launch_bounds__(256) void attention_tile_join_kernel(AttnArgs a) {
         for (int d = 1; d < 16; d *= 2) part += __shfl_xor(part, d, kWave);
         sum = fmaf(sum, shrink, quads_sum(part));
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] *= shrink;
+        for (int e = 0; e < E; ++e) acc[e] = times_unless_odd(shrink, acc[e]);
         const float* src = a.part_o + ((size_t)c0 * stride + at) * D + lane * E;
         for (int c = 0; c < n; c += kAtOnce) {
             float v[kAtOnce][E];
@@ -819,7 +870,7 @@ __global__ __launch_bounds__(256) void attention_tile_join_kernel(AttnArgs a) {
             for (int i = 0; i < kAtOnce; ++i) {
                 const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), min(c + i, n - 1)));
 #pragma unroll
-                for (int e = 0; e < E; ++e) acc[e] = c + i < n ? fmaf(v[i][e], f, acc[e]) : acc[e];
+                for (int e = 0; e < E; ++e) acc[e] = c + i < n ? acc[e] + times_unless_odd(f, v[i][e]) : acc[e];
             }
         }
     }

@@ -68,3 +68,64 @@ def test_a_long_tail_beside_a_dominant_key(form, mass, d):
     ref = B.attention(q[at, head].cpu().numpy(), k[:, head].cpu().numpy(), v[:, head].cpu().numpy(), [0, 3], [0], [keys], d,
                       float(np.float32(scale)), False, np.zeros((3, d)))
     check(got[at, head], ref, "tail")
+
+
+@pytest.mark.parametrize("seqs", [[(1, 700), (1, 40), (1, 1)], [(100, 100), (70, 200)], [(70, 6000)], [(3, 20000)], [(40, 9000), (1, 3000)]],
+                         ids=["singles", "prompts", "chunk", "far", "beside"])
+@pytest.mark.parametrize("causal", [True, False])
+@HEADS
+def test_infinities_among_the_values_a_row_sees(seqs, causal, hq, hk, d):
+    # however small the key's probability, wherever it lies: its column is infinite (NaN for two of unlike sign and for a NaN), the other
+    # columns are as ever.  Scores of some hundreds, so that most probabilities vanish.
+    c = make(seqs, hq, hk, d, 79, gap=5)
+    c["q"] = c["q"] * 8
+    g = torch.Generator().manual_seed(83)
+    ref = oracle(c, causal, scale=0.7)
+    odd = torch.zeros_like(c["v"])
+    for (n, m), start in zip(seqs, c["starts"]):
+        place = torch.randint(0, m, (6,), generator=g)
+        for j, x in zip(place.tolist(), (float("inf"), float("-inf"), float("inf"), float("nan"), float("-inf"), float("inf"))):
+            odd[start + j, torch.randint(0, hk * d, (9,), generator=g)] = x
+    late = [start + m - 1 for (_, m), start in zip(seqs, c["starts"])]
+    odd[late, 5] = float("inf")
+    c["v"] = torch.where(odd != 0, odd, c["v"])
+    got = run(c, causal, scale=0.7).cpu().double().numpy()
+    odd = odd.numpy().astype(np.float64)
+    want, bound = ref[0].copy(), ref[1].copy()
+    for (n, m), start, q0 in zip(seqs, c["starts"], c["off"]):
+        for i in range(n):
+            seen = i + m - n + 1 if causal else m
+            with np.errstate(invalid="ignore"):
+                w = np.repeat(odd[start : start + seen].sum(0).reshape(hk, 1, d), hq // hk, 1).reshape(-1)
+            hit = w != 0
+            # (two of unlike sign: NaN + anything, as it should)
+            assert np.array_equal(got[q0 + i][hit], w[hit], equal_nan=True), (n, m, i)
+            assert (np.abs(got[q0 + i][~hit] - want[q0 + i][~hit]) <= bound[q0 + i][~hit]).all(), (n, m, i)
+
+
+@SEQS
+@HEADS
+def test_an_infinity_behind_a_score_of_minus_infinity(seqs, hq, hk, d):
+    # the formula's 0 * infinity in its column; a finite value there does not count
+    c = make(seqs, hq, hk, d, 89)
+    c["q"][:, ::d] = c["q"][:, ::d].abs() + 0.1
+    ref = oracle(c, False)
+    gone = [start + m // 2 for (_, m), start in zip(seqs, c["starts"])]
+    for j in gone:
+        c["k"][j, ::d] = float("-inf")
+    base = {**c, "k": c["k"].clone()}
+    base["k"][gone] = 0.0
+    c["v"][gone, 3] = float("inf")
+    c["v"][gone, 4] = 60000.0
+    keep = torch.ones(len(c["k"]), dtype=torch.bool)
+    keep[gone] = False
+    # the oracle without those keys
+    at = np.cumsum(keep.numpy()) - 1
+    less = {**c, "k": c["k"][keep], "v": c["v"][keep], "starts": [int(at[s]) for s in c["starts"]], "lens": [m - 1 for m in c["lens"]]}
+    ref = oracle(less, False)
+    got = run(c, False)
+    cols = torch.ones(hq * d, dtype=torch.bool)
+    for h in range(hq // hk):
+        cols[h * d + 3] = False
+    assert torch.isnan(got[:, (~cols).to(DEV)]).all()
+    check(got[:, cols.to(DEV)], (ref[0][:, cols.numpy()], ref[1][:, cols.numpy()]), "the other columns")
