@@ -116,17 +116,18 @@ __device__ __forceinline__ RowTile row_tile(const AttnArgs& a, int target, int r
         const int at = __builtin_ctzll(here);
         return RowTile{at, target - __builtin_amdgcn_readlane(before, at), seq_of_lane(mine, at)};
     }
-    int before = 0;
-    for (int s0 = 0; s0 < a.seqs; s0 += kWave) {
-        const Seq mine = s0 + lane < a.seqs ? seq_at(a, s0 + lane) : none;
-        const int n = row_tiles(a, mine, rows), upto = lanes_up_to(n, lane);
-        const unsigned long long past = __ballot(before + upto > target);
-        if (past) {
-            const int first = __builtin_ctzll(past);
-            return RowTile{s0 + first, target - before - __builtin_amdgcn_readlane(upto - n, first), seq_of_lane(mine, first)};
-        }
-        before += __builtin_amdgcn_readlane(upto, kWave - 1);
+    // More of them: sequence s has the numbers from q_offsets[s] * group / rows + s on, as many as its rows can need and no more in all than
+    // the grid has, so that a search finds it in as many steps as the number of sequences has bits (a walk over all of them in each of a
+    // grid's workgroups would take their square).
+    auto begin = [&](int s) { return (int)((long long)min(max(a.q_offsets[s], 0), a.M) * a.group / rows) + s; };
+    int low = 0, past = a.seqs;
+    while (past - low > 1) {
+        const int mid = low + (past - low) / 2;
+        (begin(mid) <= target ? low : past) = mid;
     }
+    const Seq s = seq_at(a, low);
+    const int tile = target - begin(low);
+    if (tile >= 0 && tile < row_tiles(a, s, rows)) return RowTile{low, tile, s};
     return RowTile{-1, 0, none};
 }
 
@@ -468,15 +469,15 @@ __device__ __forceinline__ int few_v_chunk(int r, int c) {  // 8 rows, two chunk
 constexpr int kPiece = 6;
 struct Deal {
     int per;               // numbers of a workgroup
-    int seq, tiles, begin; // the sequence asked for (seqs: there is none), its tiles, the first number of it
+    int seq, tiles, begin; // the sequence (seqs: there is none), its tiles, the first number of it
     Seq s;
 };
 __device__ __forceinline__ int few_tiles(const AttnArgs& a, const Seq& s) {
     const int rows = s.qlen * a.group;
     return rows == 0 || rows > a.few_rows ? 0 : max((s.kvlen + kFewKeys - 1) / kFewKeys, 1);  // (rows without keys are written, too)
 }
-// By a wave: sequence `seq`, or (seq < 0) the one that holds the first tile of `slot`.
-__device__ __forceinline__ Deal few_deal(const AttnArgs& a, int slot, int seq) {
+// By a wave: the sequence that holds the first number of `slot`.
+__device__ __forceinline__ Deal few_deal(const AttnArgs& a, int slot) {
     const int lane = threadIdx.x & (kWave - 1);
     const Seq none{0, 0, 0, 0};
     const Seq mine0 = lane < a.seqs ? seq_at(a, lane) : none;
@@ -494,7 +495,7 @@ __device__ __forceinline__ Deal few_deal(const AttnArgs& a, int slot, int seq) {
     for (int s0 = 0; s0 < a.seqs; s0 += kWave) {
         const Seq mine = s0 == 0 ? mine0 : s0 + lane < a.seqs ? seq_at(a, s0 + lane) : none;
         const int n = numbers(mine), upto = lanes_up_to(n, lane);
-        const unsigned long long hit = __ballot(seq < 0 ? before + upto > want : s0 + lane == seq);
+        const unsigned long long hit = __ballot(before + upto > want);
         if (hit) {
             const int at = __builtin_ctzll(hit);
             d.seq = s0 + at;
@@ -507,6 +508,22 @@ __device__ __forceinline__ Deal few_deal(const AttnArgs& a, int slot, int seq) {
     }
     d.seq = a.seqs, d.tiles = 0, d.begin = before, d.s = none;
     return d;
+}
+// By a wave: the next sequence from `seq` on that this kernel has (seqs: there is none), with its tiles.
+__device__ __forceinline__ int few_next(const AttnArgs& a, int seq, Seq* s, int* tiles) {
+    const int lane = threadIdx.x & (kWave - 1);
+    for (; seq < a.seqs; seq += kWave) {
+        const Seq mine = seq + lane < a.seqs ? seq_at(a, seq + lane) : Seq{0, 0, 0, 0};
+        const int n = few_tiles(a, mine);
+        const unsigned long long some = __ballot(n > 0);
+        if (some) {
+            const int at = __builtin_ctzll(some);
+            *s = seq_of_lane(mine, at);
+            *tiles = __builtin_amdgcn_readlane(n, at);
+            return seq + at;
+        }
+    }
+    return a.seqs;
 }
 // Where the piece of a sequence that begins in a run's middle (first: at the sequence's beginning) lies in the workspace, in rows.
 __device__ __forceinline__ size_t piece_at(const AttnArgs& a, int slot, bool first, int head) {
@@ -527,7 +544,7 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(RB * 
     // (heads side by side: with 8 or 32 of them the workgroups i, i + 8, ... of an XCD read the same heads' columns; the heads of a run
     // on one XCD instead take 183 us where this takes 176, 1.07 GB)
     const int slot = blockIdx.x / a.heads_kv, head = blockIdx.x % a.heads_kv;
-    const Deal deal = few_deal(a, slot, -1);
+    const Deal deal = few_deal(a, slot);
     int seq = deal.seq, tiles = deal.tiles, begin = deal.begin, at = slot * deal.per;
     const int end = at + deal.per;
     Seq s = deal.s;
@@ -542,14 +559,6 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(RB * 
     const float factor = a.scale * 1.44269504088896340736f;
 
     while (seq < a.seqs && at < end) {
-    if (at == begin && seq != deal.seq) {
-        s = seq_at(a, seq);
-        tiles = few_tiles(a, s);
-        if (tiles == 0) {
-            ++seq;
-            continue;
-        }
-    }
     const int rows = s.qlen * a.group;
     const int t0 = max(at - begin - kPiece, 0), t1 = min(end - begin - kPiece, tiles);
     if (t1 <= t0) break;  // (the run ends in front of the sequence's first tile)
@@ -762,18 +771,19 @@ __global__ __launch_bounds__(NW* kWave) __attribute__((amdgpu_waves_per_eu(RB * 
     __syncthreads();  // (the next piece's tiles go where the partial results were)
     begin += kPiece + tiles;
     at = begin;
-    ++seq;
+    if (at < end) seq = few_next(a, seq + 1, &s, &tiles);
     }
 }
 
-// The pieces of a sequence that several workgroups had, joined in their order: a workgroup for each sequence and key head.
+// The pieces of a sequence that several workgroups had, joined in their order: a workgroup for each slot but the first and key head,
+// which has the sequence whose last piece is that slot's.
 template <int D>
 __global__ __launch_bounds__(256) void attention_few_join_kernel(AttnArgs a) {
-    const int seq = blockIdx.x / a.heads_kv, head = blockIdx.x % a.heads_kv;
-    const Deal d = few_deal(a, 0, seq);
+    const int slot = 1 + blockIdx.x / a.heads_kv, head = blockIdx.x % a.heads_kv;
+    const Deal d = few_deal(a, slot);
     if (d.tiles == 0) return;
     const int first = (d.begin + kPiece) / d.per, last = (d.begin + kPiece + d.tiles - 1) / d.per;
-    if (first == last) return;  // (written already)
+    if (first == last || last != slot) return;  // (written already, or another workgroup's)
     const Seq s = d.s;
     const int rows = s.qlen * a.group;
     for (int i = threadIdx.x; i < rows * (D / 4); i += 256) {
@@ -894,7 +904,7 @@ hipError_t launch_few(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) 
     hipLaunchKernelGGL(kernel, dim3((unsigned)(a.slots * a.heads_kv)), dim3(NW * kWave), bytes, stream, a);
     const hipError_t launched = hipGetLastError();
     if (launched != hipSuccess || !p.few_cut) return launched;
-    hipLaunchKernelGGL((attention_few_join_kernel<D>), dim3((unsigned)(a.seqs * a.heads_kv)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((attention_few_join_kernel<D>), dim3((unsigned)((a.slots - 1) * a.heads_kv)), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 

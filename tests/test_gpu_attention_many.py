@@ -58,3 +58,24 @@ def test_pieces_of_a_chunk_among_many_sequences():
     seqs = [(0, 5), (1, 40)] * 40 + [(30, 21000)] + [(1, 300)] * 20
     c = make(seqs, 8, 1, 64, 101)
     check(run(c, True), oracle(c, True), "many")
+
+
+@pytest.mark.parametrize("some", [{0: (1, 900), 70000: (1, 5000), 70001: (1, 3), 149999: (1, 2500)}, {3: (1, 40), 70000: (100, 700), 149999: (90, 90)},
+                                  {149999: (30, 21000)}], ids=["singles", "prompts", "chunk"])
+def test_a_hundred_thousand_sequences_without_rows(some):
+    # between the few that have some: a look at all of them in every workgroup, or one after the other, would take seconds
+    n = 150000
+    c = make([some[i] for i in sorted(some)], 4, 2, 64, 103, gap=2, tail=1)
+    for x, rest in (("off", None), ("starts", 7), ("lens", 11)):
+        v = torch.full((n,), 0 if rest is None else rest)
+        for i, s in enumerate(sorted(some)):
+            v[s] = some[s][0] if rest is None else c[x][i]
+        big = torch.cat([torch.zeros(1, dtype=v.dtype), v.cumsum(0)]) if rest is None else v
+        c["big_" + x] = big.to(DEV, torch.int64 if x == "starts" else torch.int32)
+    torch.cuda.synchronize()
+    e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    e0.record()
+    got = run(c, True, q_offsets=c["big_off"], kv_starts=c["big_starts"], kv_lens=c["big_lens"])
+    e1.record()
+    check(got, oracle(c, True), "some")
+    print("many sequences: %.2f ms" % e0.elapsed_time(e1), flush=True)
