@@ -311,11 +311,11 @@ def is_quantize_weights_int4_group(w, group: int, alpha_log2: int, scale_mode: i
     if group <= 0 or K % group != 0:
         raise IntScaleError("is_quantize_weights_int4_group", IS_ERR_INVALID_ARG)
     dev = w.device
-    q = torch.empty((N, K // 2), dtype=torch.uint8, device=dev)
-    s = torch.empty((N, K // group), dtype=torch.float32, device=dev)
-    si = torch.empty((N, K // group), dtype=torch.int32, device=dev)
-    c = torch.empty((N,), dtype=torch.float32, device=dev)
-    a_dev = torch.empty((4,), dtype=torch.int32, device=dev)
+    q = _empty((N, K // 2), torch.uint8, dev, stream)
+    s = _empty((N, K // group), torch.float32, dev, stream)
+    si = _empty((N, K // group), torch.int32, dev, stream)
+    c = _empty((N,), torch.float32, dev, stream)
+    a_dev = _empty((4,), torch.int32, dev, stream)
     st = load_library().is_quantize_weights_int4_group(_p(w), N, K, group, alpha_log2, scale_mode, _p(q), _p(s), _p(si),
                                                       _p(c), _p(a_dev), _stream_handle(stream))
     _check("is_quantize_weights_int4_group", st)
@@ -327,9 +327,9 @@ def is_quantize_act_int8_token(x, xq=None, a_scale=None, stream=None):
     M, K = x.shape
     _require(x, torch.float16, (M, K), "x")
     if xq is None:
-        xq = torch.empty((M, K), dtype=torch.int8, device=x.device)
+        xq = _empty((M, K), torch.int8, x.device, stream)
     if a_scale is None:
-        a_scale = torch.empty((M,), dtype=torch.float32, device=x.device)
+        a_scale = _empty((M,), torch.float32, x.device, stream)
     _require(xq, torch.int8, (M, K), "xq")
     _require(a_scale, torch.float32, (M,), "a_scale")
     st = load_library().is_quantize_act_int8_token(_p(x), M, K, _p(xq), _p(a_scale), _stream_handle(stream))
@@ -343,9 +343,9 @@ def is_rmsnorm_quantize_act_int8_token(x, gamma, eps: float, xq=None, a_scale=No
     _require(x, torch.float16, (M, K), "x")
     _require(gamma, torch.float16, (K,), "gamma")
     if xq is None:
-        xq = torch.empty((M, K), dtype=torch.int8, device=x.device)
+        xq = _empty((M, K), torch.int8, x.device, stream)
     if a_scale is None:
-        a_scale = torch.empty((M,), dtype=torch.float32, device=x.device)
+        a_scale = _empty((M,), torch.float32, x.device, stream)
     _require(xq, torch.int8, (M, K), "xq")
     _require(a_scale, torch.float32, (M,), "a_scale")
     st = load_library().is_rmsnorm_quantize_act_int8_token(_p(x), _p(gamma), float(eps), M, K, _p(xq), _p(a_scale),
@@ -360,9 +360,9 @@ def is_silu_mul_quantize_act_int8_token(gate_up, xq=None, a_scale=None, stream=N
     inter = two_inter // 2
     _require(gate_up, torch.float16, (M, 2 * inter), "gate_up")
     if xq is None:
-        xq = torch.empty((M, inter), dtype=torch.int8, device=gate_up.device)
+        xq = _empty((M, inter), torch.int8, gate_up.device, stream)
     if a_scale is None:
-        a_scale = torch.empty((M,), dtype=torch.float32, device=gate_up.device)
+        a_scale = _empty((M,), torch.float32, gate_up.device, stream)
     _require(xq, torch.int8, (M, inter), "xq")
     _require(a_scale, torch.float32, (M,), "a_scale")
     st = load_library().is_silu_mul_quantize_act_int8_token(_p(gate_up), M, inter, _p(xq), _p(a_scale),
@@ -379,34 +379,41 @@ def is_gemm_grouped_workspace_bytes(E: int, M_total: int, N: int, K: int, group:
     return int(load_library().is_gemm_grouped_workspace_bytes(E, M_total, N, K, group))
 
 
-def _workspace(query, sizes, device, workspace):
-    """The caller's workspace, or one of the size that `query(*sizes)` asks for (the library checks the caller's itself)."""
+def _on_stream(make, shape, dtype, device, stream):
+    """make(shape) for a call on `stream` (None: the current one), from that stream's memory and with its fill queued there.  What the
+    current stream's allocator has free may still be in use by work queued on that, and a fill there would be queued inside the call,
+    where no caller can order it before the call's kernels."""
+    if stream is None:
+        return make(shape, dtype=dtype, device=device)
+    with _torch().cuda.stream(stream):
+        return make(shape, dtype=dtype, device=device)
+
+
+def _empty(shape, dtype, device, stream):
+    """A call's new output."""
+    t = _on_stream(_torch().empty, shape, dtype, device, stream)
+    if stream is not None:
+        t.record_stream(_torch().cuda.current_stream())  # (the caller's, who reads it there once it has waited)
+    return t
+
+
+def _zeros(shape, dtype, device, stream):
+    t = _on_stream(_torch().zeros, shape, dtype, device, stream)
+    if stream is not None:
+        t.record_stream(_torch().cuda.current_stream())
+    return t
+
+
+def _workspace(query, sizes, device, workspace, stream, zero=False):
+    """The caller's workspace, or one of the size that `query(*sizes)` asks for (the library checks the caller's itself).  The latter goes
+    back to its stream's memory when the call returns, where later calls are ordered after its kernels."""
     if workspace is not None:
         return workspace, workspace.numel() * workspace.element_size()
     nbytes = query(*sizes)
     if nbytes == 0:
         return None, 0
-    ws = _torch().empty((nbytes,), dtype=_torch().uint8, device=device)
-    return ws, nbytes
-
-
-def _zeros(shape, dtype, device, stream):
-    """A zero-filled tensor for a call on `stream` (None: the current one).  It is allocated and filled on that stream: a fill on
-    the current one would be queued inside the call, where no caller can order it before the call's kernels."""
     torch = _torch()
-    if stream is None:
-        return torch.zeros(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        t = torch.zeros(shape, dtype=dtype, device=device)
-    t.record_stream(torch.cuda.current_stream())  # (whoever gets it reads it there, most likely)
-    return t
-
-
-def _release_workspace(ws, workspace, stream) -> None:
-    """A workspace this module allocated goes back to torch's allocator when the call returns, while the kernels may
-    still be queued: tell the allocator which stream uses it, so the block is not handed out on another stream early."""
-    if ws is not None and workspace is None and stream is not None and hasattr(stream, "cuda_stream"):
-        ws.record_stream(stream)
+    return _on_stream(torch.zeros if zero else torch.empty, (nbytes,), torch.uint8, device, stream), nbytes
 
 
 def is_gemm_w4a8_intscale(xq, a_scale, qweight, scale_i32, chan_scale, group: int, alpha_log2: int, out=None,
@@ -422,18 +429,17 @@ def is_gemm_w4a8_intscale(xq, a_scale, qweight, scale_i32, chan_scale, group: in
     if chan_scale is not None:
         _require(chan_scale, torch.float32, (N,), "chan_scale")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=xq.device)
+        out = _empty((M, N), torch.float16, xq.device, stream)
     _require(out, torch.float16, (M, N), "out")
     if acc_out is None and want_acc:
-        acc_out = torch.empty((M, N), dtype=torch.int32, device=xq.device)
+        acc_out = _empty((M, N), torch.int32, xq.device, stream)
     if acc_out is not None:
         _require(acc_out, torch.int32, (M, N), "acc_out")
-    ws, ws_bytes = _workspace(is_gemm_workspace_bytes, (M, N, K, group), xq.device, workspace)
+    ws, ws_bytes = _workspace(is_gemm_workspace_bytes, (M, N, K, group), xq.device, workspace, stream)
     st = load_library().is_gemm_w4a8_intscale(_p(xq), _p(a_scale), _p(qweight), _p(scale_i32), _p(chan_scale), M, N, K,
                                              group, alpha_log2, _p(out), _p(acc_out), _p(ws), ws_bytes,
                                              _stream_handle(stream))
     _check("is_gemm_w4a8_intscale", st)
-    _release_workspace(ws, workspace, stream)
     return out, acc_out
 
 
@@ -446,13 +452,12 @@ def is_gemm_w4a8_floatscale(xq, a_scale, qweight, scale_f32, group: int, out=Non
     _require(qweight, torch.uint8, (N, K // 2), "qweight")
     _require(scale_f32, torch.float32, (N, K // group), "scale_f32")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=xq.device)
+        out = _empty((M, N), torch.float16, xq.device, stream)
     _require(out, torch.float16, (M, N), "out")
-    ws, ws_bytes = _workspace(is_gemm_workspace_bytes, (M, N, K, group), xq.device, workspace)
+    ws, ws_bytes = _workspace(is_gemm_workspace_bytes, (M, N, K, group), xq.device, workspace, stream)
     st = load_library().is_gemm_w4a8_floatscale(_p(xq), _p(a_scale), _p(qweight), _p(scale_f32), M, N, K, group,
                                                _p(out), _p(ws), ws_bytes, _stream_handle(stream))
     _check("is_gemm_w4a8_floatscale", st)
-    _release_workspace(ws, workspace, stream)
     return out
 
 
@@ -472,18 +477,17 @@ def is_linear_w4a8_intscale(x, qweight, scale_i32, chan_scale, group: int, alpha
     if chan_scale is not None:
         _require(chan_scale, torch.float32, (N,), "chan_scale")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=x.device)
+        out = _empty((M, N), torch.float16, x.device, stream)
     _require(out, torch.float16, (M, N), "out")
     if acc_out is None and want_acc:
-        acc_out = torch.empty((M, N), dtype=torch.int32, device=x.device)
+        acc_out = _empty((M, N), torch.int32, x.device, stream)
     if acc_out is not None:
         _require(acc_out, torch.int32, (M, N), "acc_out")
-    ws, ws_bytes = _workspace(is_linear_workspace_bytes, (M, N, K, group), x.device, workspace)
+    ws, ws_bytes = _workspace(is_linear_workspace_bytes, (M, N, K, group), x.device, workspace, stream)
     st = load_library().is_linear_w4a8_intscale(_p(x), _p(qweight), _p(scale_i32), _p(chan_scale), M, N, K, group,
                                                alpha_log2, _p(out), _p(acc_out), _p(ws), ws_bytes,
                                                _stream_handle(stream))
     _check("is_linear_w4a8_intscale", st)
-    _release_workspace(ws, workspace, stream)
     return out, acc_out
 
 
@@ -495,13 +499,12 @@ def is_linear_w4a8_floatscale(x, qweight, scale_f32, group: int, out=None, works
     _require(qweight, torch.uint8, (N, K // 2), "qweight")
     _require(scale_f32, torch.float32, (N, K // group), "scale_f32")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=x.device)
+        out = _empty((M, N), torch.float16, x.device, stream)
     _require(out, torch.float16, (M, N), "out")
-    ws, ws_bytes = _workspace(is_linear_workspace_bytes, (M, N, K, group), x.device, workspace)
+    ws, ws_bytes = _workspace(is_linear_workspace_bytes, (M, N, K, group), x.device, workspace, stream)
     st = load_library().is_linear_w4a8_floatscale(_p(x), _p(qweight), _p(scale_f32), M, N, K, group, _p(out), _p(ws),
                                                  ws_bytes, _stream_handle(stream))
     _check("is_linear_w4a8_floatscale", st)
-    _release_workspace(ws, workspace, stream)
     return out
 
 
@@ -514,11 +517,11 @@ def is_quantize_weights_int8_group(w, group: int, alpha_log2: int, scale_mode: i
     if group <= 0 or K % group != 0:
         raise IntScaleError("is_quantize_weights_int8_group", IS_ERR_INVALID_ARG)
     dev = w.device
-    q = torch.empty((N, K), dtype=torch.int8, device=dev)
-    s = torch.empty((N, K // group), dtype=torch.float32, device=dev)
-    si = torch.empty((N, K // group), dtype=torch.int32, device=dev)
-    c = torch.empty((N,), dtype=torch.float32, device=dev)
-    a_dev = torch.empty((4,), dtype=torch.int32, device=dev)
+    q = _empty((N, K), torch.int8, dev, stream)
+    s = _empty((N, K // group), torch.float32, dev, stream)
+    si = _empty((N, K // group), torch.int32, dev, stream)
+    c = _empty((N,), torch.float32, dev, stream)
+    a_dev = _empty((4,), torch.int32, dev, stream)
     st = load_library().is_quantize_weights_int8_group(_p(w), N, K, group, alpha_log2, scale_mode, _p(q), _p(s), _p(si),
                                                       _p(c), _p(a_dev), _stream_handle(stream))
     _check("is_quantize_weights_int8_group", st)
@@ -542,18 +545,17 @@ def is_gemm_w8a8_intscale(xq, a_scale, qweight8, scale_i32, chan_scale, group: i
     if chan_scale is not None:
         _require(chan_scale, torch.float32, (N,), "chan_scale")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=xq.device)
+        out = _empty((M, N), torch.float16, xq.device, stream)
     _require(out, torch.float16, (M, N), "out")
     if acc_out is None and want_acc:
-        acc_out = torch.empty((M, N), dtype=torch.int32, device=xq.device)
+        acc_out = _empty((M, N), torch.int32, xq.device, stream)
     if acc_out is not None:
         _require(acc_out, torch.int32, (M, N), "acc_out")
-    ws, ws_bytes = _workspace(is_gemm_w8a8_workspace_bytes, (M, N, K, group), xq.device, workspace)
+    ws, ws_bytes = _workspace(is_gemm_w8a8_workspace_bytes, (M, N, K, group), xq.device, workspace, stream)
     st = load_library().is_gemm_w8a8_intscale(_p(xq), _p(a_scale), _p(qweight8), _p(scale_i32), _p(chan_scale), M, N, K,
                                              group, alpha_log2, _p(out), _p(acc_out), _p(ws), ws_bytes,
                                              _stream_handle(stream))
     _check("is_gemm_w8a8_intscale", st)
-    _release_workspace(ws, workspace, stream)
     return out, acc_out
 
 
@@ -566,13 +568,12 @@ def is_gemm_w8a8_floatscale(xq, a_scale, qweight8, scale_f32, group: int, out=No
     _require(qweight8, torch.int8, (N, K), "qweight8")
     _require(scale_f32, torch.float32, (N, K // group), "scale_f32")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=xq.device)
+        out = _empty((M, N), torch.float16, xq.device, stream)
     _require(out, torch.float16, (M, N), "out")
-    ws, ws_bytes = _workspace(is_gemm_w8a8_workspace_bytes, (M, N, K, group), xq.device, workspace)
+    ws, ws_bytes = _workspace(is_gemm_w8a8_workspace_bytes, (M, N, K, group), xq.device, workspace, stream)
     st = load_library().is_gemm_w8a8_floatscale(_p(xq), _p(a_scale), _p(qweight8), _p(scale_f32), M, N, K, group,
                                                _p(out), _p(ws), ws_bytes, _stream_handle(stream))
     _check("is_gemm_w8a8_floatscale", st)
-    _release_workspace(ws, workspace, stream)
     return out
 
 
@@ -592,14 +593,13 @@ def is_gemm_w4a8_intscale_safe(xq, a_scale, qweight, scale_i32, chan_scale, grou
     if chan_scale is not None:
         _require(chan_scale, torch.float32, (N,), "chan_scale")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=xq.device)
+        out = _empty((M, N), torch.float16, xq.device, stream)
     _require(out, torch.float16, (M, N), "out")
-    ws, ws_bytes = _workspace(is_gemm_safe_workspace_bytes, (M, N, K, group), xq.device, workspace)
+    ws, ws_bytes = _workspace(is_gemm_safe_workspace_bytes, (M, N, K, group), xq.device, workspace, stream)
     st = load_library().is_gemm_w4a8_intscale_safe(_p(xq), _p(a_scale), _p(qweight), _p(scale_i32), _p(chan_scale), M,
                                                   N, K, group, alpha_log2, _p(out), _p(ws), ws_bytes,
                                                   _stream_handle(stream))
     _check("is_gemm_w4a8_intscale_safe", st)
-    _release_workspace(ws, workspace, stream)
     return out
 
 
@@ -609,7 +609,7 @@ def is_intscale_overflow_bound(scale_i32, group: int, bound=None, stream=None):
     N, NG = scale_i32.shape
     _require(scale_i32, torch.int32, (N, NG), "scale_i32")
     if bound is None:
-        bound = torch.empty((1,), dtype=torch.int64, device=scale_i32.device)
+        bound = _empty((1,), torch.int64, scale_i32.device, stream)
     _require(bound, torch.int64, (1,), "bound")
     st = load_library().is_intscale_overflow_bound(_p(scale_i32), N, NG * group, group, _p(bound), _stream_handle(stream))
     _check("is_intscale_overflow_bound", st)
@@ -630,16 +630,15 @@ def is_gemm_w4a8_intscale_grouped(xq, a_scale, qweight, scale_i32, chan_scale, r
     if chan_scale is not None:
         _require(chan_scale, torch.float32, (E, N), "chan_scale")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=xq.device)
+        out = _empty((M, N), torch.float16, xq.device, stream)
     _require(out, torch.float16, (M, N), "out")
     if acc_out is None and want_acc:
-        acc_out = torch.empty((M, N), dtype=torch.int32, device=xq.device)
-    ws, ws_bytes = _workspace(is_gemm_grouped_workspace_bytes, (E, M, N, K, group), xq.device, workspace)
+        acc_out = _empty((M, N), torch.int32, xq.device, stream)
+    ws, ws_bytes = _workspace(is_gemm_grouped_workspace_bytes, (E, M, N, K, group), xq.device, workspace, stream)
     st = load_library().is_gemm_w4a8_intscale_grouped(_p(xq), _p(a_scale), _p(qweight), _p(scale_i32), _p(chan_scale),
                                                      _p(row_offsets), E, M, N, K, group, alpha_log2, _p(out),
                                                      _p(acc_out), _p(ws), ws_bytes, _stream_handle(stream))
     _check("is_gemm_w4a8_intscale_grouped", st)
-    _release_workspace(ws, workspace, stream)
     return out, acc_out
 
 
@@ -654,14 +653,13 @@ def is_gemm_w4a8_floatscale_grouped(xq, a_scale, qweight, scale_f32, row_offsets
     _require(scale_f32, torch.float32, (E, N, K // group), "scale_f32")
     _require(row_offsets, torch.int32, (E + 1,), "row_offsets")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=xq.device)
+        out = _empty((M, N), torch.float16, xq.device, stream)
     _require(out, torch.float16, (M, N), "out")
-    ws, ws_bytes = _workspace(is_gemm_grouped_workspace_bytes, (E, M, N, K, group), xq.device, workspace)
+    ws, ws_bytes = _workspace(is_gemm_grouped_workspace_bytes, (E, M, N, K, group), xq.device, workspace, stream)
     st = load_library().is_gemm_w4a8_floatscale_grouped(_p(xq), _p(a_scale), _p(qweight), _p(scale_f32),
                                                        _p(row_offsets), E, M, N, K, group, _p(out), _p(ws), ws_bytes,
                                                        _stream_handle(stream))
     _check("is_gemm_w4a8_floatscale_grouped", st)
-    _release_workspace(ws, workspace, stream)
     return out
 
 
@@ -713,8 +711,8 @@ def is_prepack_w4(qweight, scale, group: int, stream=None) -> PackedWeights:
     wb, sb = int(lib.is_prepack_w4_weight_bytes(N, K)), int(lib.is_prepack_w4_scale_bytes(N, K, group))
     if wb == 0 or sb == 0:
         raise IntScaleError("is_prepack_w4", IS_ERR_UNSUPPORTED)
-    wpack = torch.empty((wb,), dtype=torch.uint8, device=qweight.device)
-    spack = torch.empty((sb,), dtype=torch.uint8, device=qweight.device)
+    wpack = _empty((wb,), torch.uint8, qweight.device, stream)
+    spack = _empty((sb,), torch.uint8, qweight.device, stream)
     is_float = scale.dtype == torch.float32
     st = lib.is_prepack_w4(_p(qweight), None if is_float else _p(scale), _p(scale) if is_float else None, N, K, group,
                            _p(wpack), _p(spack), _stream_handle(stream))
@@ -753,8 +751,8 @@ def is_prepack_w4_experts(qweight, scale, group: int, stream=None) -> PackedExpe
     wb, sb = int(lib.is_prepack_w4_weight_bytes(N, K)), int(lib.is_prepack_w4_scale_bytes(N, K, group))
     if wb == 0 or sb == 0:
         raise IntScaleError("is_prepack_w4", IS_ERR_UNSUPPORTED)
-    wpack = torch.empty((E, wb), dtype=torch.uint8, device=qweight.device)
-    spack = torch.empty((E, sb), dtype=torch.uint8, device=qweight.device)
+    wpack = _empty((E, wb), torch.uint8, qweight.device, stream)
+    spack = _empty((E, sb), torch.uint8, qweight.device, stream)
     is_float = scale.dtype == torch.float32
     for e in range(E):
         st = lib.is_prepack_w4(_p(qweight[e]), None if is_float else _p(scale[e]), _p(scale[e]) if is_float else None, N, K,
@@ -781,18 +779,17 @@ def is_gemm_w4a8_intscale_grouped_prepacked(xq, a_scale, packed: PackedExperts, 
     if chan_scale is not None:
         _require(chan_scale, torch.float32, (E, N), "chan_scale")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=xq.device)
+        out = _empty((M, N), torch.float16, xq.device, stream)
     _require(out, torch.float16, (M, N), "out")
     if acc_out is None and want_acc:
-        acc_out = torch.empty((M, N), dtype=torch.int32, device=xq.device)
+        acc_out = _empty((M, N), torch.int32, xq.device, stream)
     if acc_out is not None:
         _require(acc_out, torch.int32, (M, N), "acc_out")
-    ws, ws_bytes = _workspace(is_gemm_grouped_prepacked_workspace_bytes, (E, M, N, K, group), xq.device, workspace)
+    ws, ws_bytes = _workspace(is_gemm_grouped_prepacked_workspace_bytes, (E, M, N, K, group), xq.device, workspace, stream)
     st = load_library().is_gemm_w4a8_intscale_grouped_prepacked(
         _p(xq), _p(a_scale), _p(packed.wpack), _p(packed.spack), _p(chan_scale), _p(row_offsets), E, M, N, K, group,
         alpha_log2, _p(out), _p(acc_out), _p(ws), ws_bytes, _stream_handle(stream))
     _check("is_gemm_w4a8_intscale_grouped_prepacked", st)
-    _release_workspace(ws, workspace, stream)
     return out, acc_out
 
 
@@ -807,14 +804,13 @@ def is_gemm_w4a8_floatscale_grouped_prepacked(xq, a_scale, packed: PackedExperts
     _require(a_scale, torch.float32, (M,), "a_scale")
     _require(row_offsets, torch.int32, (E + 1,), "row_offsets")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=xq.device)
+        out = _empty((M, N), torch.float16, xq.device, stream)
     _require(out, torch.float16, (M, N), "out")
-    ws, ws_bytes = _workspace(is_gemm_grouped_prepacked_workspace_bytes, (E, M, N, K, group), xq.device, workspace)
+    ws, ws_bytes = _workspace(is_gemm_grouped_prepacked_workspace_bytes, (E, M, N, K, group), xq.device, workspace, stream)
     st = load_library().is_gemm_w4a8_floatscale_grouped_prepacked(
         _p(xq), _p(a_scale), _p(packed.wpack), _p(packed.spack), _p(row_offsets), E, M, N, K, group, _p(out), _p(ws),
         ws_bytes, _stream_handle(stream))
     _check("is_gemm_w4a8_floatscale_grouped_prepacked", st)
-    _release_workspace(ws, workspace, stream)
     return out
 
 
@@ -837,12 +833,7 @@ def is_describe_grouped_prepacked(num_experts: int, M_total: int, N: int, K: int
 
 def _zero_workspace(query, sizes, device, workspace, stream):
     """The prepacked GEMMs want their arrival counters zero: a fresh workspace is zero-filled."""
-    if workspace is not None:
-        return workspace, workspace.numel() * workspace.element_size()
-    nbytes = query(*sizes)
-    if nbytes == 0:
-        return None, 0
-    return _zeros((nbytes,), _torch().uint8, device, stream), nbytes
+    return _workspace(query, sizes, device, workspace, stream, zero=True)
 
 
 def is_gemm_w4a8_intscale_prepacked(xq, a_scale, packed: PackedWeights, chan_scale, alpha_log2: int, out=None,
@@ -858,10 +849,10 @@ def is_gemm_w4a8_intscale_prepacked(xq, a_scale, packed: PackedWeights, chan_sca
     if chan_scale is not None:
         _require(chan_scale, torch.float32, (N,), "chan_scale")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=xq.device)
+        out = _empty((M, N), torch.float16, xq.device, stream)
     _require(out, torch.float16, (M, N), "out")
     if acc_out is None and want_acc:
-        acc_out = torch.empty((M, N), dtype=torch.int32, device=xq.device)
+        acc_out = _empty((M, N), torch.int32, xq.device, stream)
     if acc_out is not None:
         _require(acc_out, torch.int32, (M, N), "acc_out")
     ws, ws_bytes = _zero_workspace(is_gemm_prepacked_workspace_bytes, (M, N, K, group), xq.device, workspace, stream)
@@ -869,7 +860,6 @@ def is_gemm_w4a8_intscale_prepacked(xq, a_scale, packed: PackedWeights, chan_sca
                                                        _p(chan_scale), M, N, K, group, alpha_log2, _p(out), _p(acc_out),
                                                        _p(ws), ws_bytes, _stream_handle(stream))
     _check("is_gemm_w4a8_intscale_prepacked", st)
-    _release_workspace(ws, workspace, stream)
     return out, acc_out
 
 
@@ -897,9 +887,9 @@ def is_prepack_w4_gate_up(qweight, scale, chan_scale, group: int, stream=None) -
     wb, sb = int(lib.is_prepack_w4_weight_bytes(N, K)), int(lib.is_prepack_w4_scale_bytes(N, K, group))
     if wb == 0 or sb == 0:
         raise IntScaleError("is_prepack_w4_gate_up", IS_ERR_UNSUPPORTED)
-    wpack = torch.empty((wb,), dtype=torch.uint8, device=qweight.device)
-    spack = torch.empty((sb,), dtype=torch.uint8, device=qweight.device)
-    cpack = None if chan_scale is None else torch.empty((N,), dtype=torch.float32, device=qweight.device)
+    wpack = _empty((wb,), torch.uint8, qweight.device, stream)
+    spack = _empty((sb,), torch.uint8, qweight.device, stream)
+    cpack = None if chan_scale is None else _empty((N,), torch.float32, qweight.device, stream)
     is_float = scale.dtype == torch.float32
     st = lib.is_prepack_w4_gate_up(_p(qweight), None if is_float else _p(scale), _p(scale) if is_float else None,
                                    _p(chan_scale), inter, K, group, _p(wpack), _p(spack), _p(cpack), _stream_handle(stream))
@@ -922,10 +912,10 @@ def is_gemm_w4a8_intscale_gate_up_silu_prepacked(xq, a_scale, gate_up: PackedGat
     _require(xq, torch.int8, (M, K), "xq")
     _require(a_scale, torch.float32, (M,), "a_scale")
     if out is None:
-        out = torch.empty((M, inter), dtype=torch.float16, device=xq.device)
+        out = _empty((M, inter), torch.float16, xq.device, stream)
     _require(out, torch.float16, (M, inter), "out")
     if acc_out is None and want_acc:
-        acc_out = torch.empty((M, 2 * inter), dtype=torch.int32, device=xq.device)
+        acc_out = _empty((M, 2 * inter), torch.int32, xq.device, stream)
     if acc_out is not None:
         _require(acc_out, torch.int32, (M, 2 * inter), "acc_out")
     ws, ws_bytes = _zero_workspace(is_gemm_gate_up_silu_prepacked_workspace_bytes, (M, inter, K, packed.group), xq.device,
@@ -934,7 +924,6 @@ def is_gemm_w4a8_intscale_gate_up_silu_prepacked(xq, a_scale, gate_up: PackedGat
         _p(xq), _p(a_scale), _p(packed.wpack), _p(packed.spack), _p(gate_up.chan_scale), M, inter, K, packed.group,
         alpha_log2, _p(out), _p(acc_out), _p(ws), ws_bytes, _stream_handle(stream))
     _check("is_gemm_w4a8_intscale_gate_up_silu_prepacked", st)
-    _release_workspace(ws, workspace, stream)
     return out, acc_out
 
 
@@ -948,7 +937,7 @@ def is_gemm_w4a8_floatscale_gate_up_silu_prepacked(xq, a_scale, gate_up: PackedG
     _require(xq, torch.int8, (M, K), "xq")
     _require(a_scale, torch.float32, (M,), "a_scale")
     if out is None:
-        out = torch.empty((M, inter), dtype=torch.float16, device=xq.device)
+        out = _empty((M, inter), torch.float16, xq.device, stream)
     _require(out, torch.float16, (M, inter), "out")
     ws, ws_bytes = _zero_workspace(is_gemm_gate_up_silu_prepacked_workspace_bytes, (M, inter, K, packed.group), xq.device,
                                    workspace, stream)
@@ -956,7 +945,6 @@ def is_gemm_w4a8_floatscale_gate_up_silu_prepacked(xq, a_scale, gate_up: PackedG
         _p(xq), _p(a_scale), _p(packed.wpack), _p(packed.spack), M, inter, K, packed.group, _p(out), _p(ws), ws_bytes,
         _stream_handle(stream))
     _check("is_gemm_w4a8_floatscale_gate_up_silu_prepacked", st)
-    _release_workspace(ws, workspace, stream)
     return out
 
 
@@ -1011,10 +999,10 @@ def is_gemm_w4a8_intscale_prepacked_prepared(a_scale, packed: PackedWeights, cha
     if chan_scale is not None:
         _require(chan_scale, torch.float32, (N,), "chan_scale")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=a_scale.device)
+        out = _empty((M, N), torch.float16, a_scale.device, stream)
     _require(out, torch.float16, (M, N), "out")
     if acc_out is None and want_acc:
-        acc_out = torch.empty((M, N), dtype=torch.int32, device=a_scale.device)
+        acc_out = _empty((M, N), torch.int32, a_scale.device, stream)
     if acc_out is not None:
         _require(acc_out, torch.int32, (M, N), "acc_out")
     st = load_library().is_gemm_w4a8_intscale_prepacked_prepared(
@@ -1032,7 +1020,7 @@ def is_gemm_w4a8_floatscale_prepacked_prepared(a_scale, packed: PackedWeights, w
         raise ValueError("packed weights: integer scales")
     _require(a_scale, torch.float32, (M,), "a_scale")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=a_scale.device)
+        out = _empty((M, N), torch.float16, a_scale.device, stream)
     _require(out, torch.float16, (M, N), "out")
     st = load_library().is_gemm_w4a8_floatscale_prepacked_prepared(
         _p(a_scale), _p(packed.wpack), _p(packed.spack), M, N, K, group, _p(out), _p(workspace), workspace.numel(),
@@ -1050,13 +1038,12 @@ def is_gemm_w4a8_floatscale_prepacked(xq, a_scale, packed: PackedWeights, out=No
     _require(xq, torch.int8, (M, K), "xq")
     _require(a_scale, torch.float32, (M,), "a_scale")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=xq.device)
+        out = _empty((M, N), torch.float16, xq.device, stream)
     _require(out, torch.float16, (M, N), "out")
     ws, ws_bytes = _zero_workspace(is_gemm_prepacked_workspace_bytes, (M, N, K, group), xq.device, workspace, stream)
     st = load_library().is_gemm_w4a8_floatscale_prepacked(_p(xq), _p(a_scale), _p(packed.wpack), _p(packed.spack), M, N,
                                                          K, group, _p(out), _p(ws), ws_bytes, _stream_handle(stream))
     _check("is_gemm_w4a8_floatscale_prepacked", st)
-    _release_workspace(ws, workspace, stream)
     return out
 
 
@@ -1072,10 +1059,10 @@ def is_linear_w4a8_intscale_prepacked(x, packed: PackedWeights, chan_scale, alph
     if chan_scale is not None:
         _require(chan_scale, torch.float32, (N,), "chan_scale")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=x.device)
+        out = _empty((M, N), torch.float16, x.device, stream)
     _require(out, torch.float16, (M, N), "out")
     if acc_out is None and want_acc:
-        acc_out = torch.empty((M, N), dtype=torch.int32, device=x.device)
+        acc_out = _empty((M, N), torch.int32, x.device, stream)
     if acc_out is not None:
         _require(acc_out, torch.int32, (M, N), "acc_out")
     ws, ws_bytes = _zero_workspace(is_linear_prepacked_workspace_bytes, (M, N, K, group), x.device, workspace, stream)
@@ -1083,7 +1070,6 @@ def is_linear_w4a8_intscale_prepacked(x, packed: PackedWeights, chan_scale, alph
                                                          K, group, alpha_log2, _p(out), _p(acc_out), _p(ws), ws_bytes,
                                                          _stream_handle(stream))
     _check("is_linear_w4a8_intscale_prepacked", st)
-    _release_workspace(ws, workspace, stream)
     return out, acc_out
 
 
@@ -1095,13 +1081,12 @@ def is_linear_w4a8_floatscale_prepacked(x, packed: PackedWeights, out=None, work
         raise ValueError("packed weights: K mismatch or integer scales")
     _require(x, torch.float16, (M, K), "x")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float16, device=x.device)
+        out = _empty((M, N), torch.float16, x.device, stream)
     _require(out, torch.float16, (M, N), "out")
     ws, ws_bytes = _zero_workspace(is_linear_prepacked_workspace_bytes, (M, N, K, group), x.device, workspace, stream)
     st = load_library().is_linear_w4a8_floatscale_prepacked(_p(x), _p(packed.wpack), _p(packed.spack), M, N, K, group,
                                                            _p(out), _p(ws), ws_bytes, _stream_handle(stream))
     _check("is_linear_w4a8_floatscale_prepacked", st)
-    _release_workspace(ws, workspace, stream)
     return out
 
 
@@ -1156,11 +1141,11 @@ def is_qk_norm_rope(q, k, positions, inv_freq, head_dim: int, gamma_q=None, gamm
     if v is None and v_out is not None:
         raise ValueError("v_out: there is no v")
     if q_out is None:
-        q_out = _torch().empty((M, wq), dtype=_half_dtype, device=q.device)
+        q_out = _empty((M, wq), _half_dtype, q.device, stream)
     if k_out is None:
-        k_out = _torch().empty((M, wk), dtype=_half_dtype, device=q.device)
+        k_out = _empty((M, wk), _half_dtype, q.device, stream)
     if v is not None and v_out is None:
-        v_out = _torch().empty((M, wk), dtype=_half_dtype, device=q.device)
+        v_out = _empty((M, wk), _half_dtype, q.device, stream)
     rows = k_out.shape[0] if kv_rows is not None else M
     ldq, ldk = _rows(q, M, wq, device, "q"), _rows(k, M, wk, device, "k")
     ldqo, ldko = _rows(q_out, M, wq, device, "q_out"), _rows(k_out, rows, wk, device, "k_out")
@@ -1209,12 +1194,11 @@ def is_attention(q, k, v, q_offsets, head_dim: int, max_q_len: int, max_kv_len: 
     if kv_lens is not None:
         _vector(kv_lens, _int32_dtype, seqs, device, "kv_lens")
     sizes = (M, seqs, max_q_len, max_kv_len, wq // head_dim, wk // head_dim, head_dim)
-    ws, ws_bytes = _workspace(is_attention_workspace_bytes, sizes, q.device, workspace)
+    ws, ws_bytes = _workspace(is_attention_workspace_bytes, sizes, q.device, workspace, stream)
     st = load_library().is_attention(_p(q), ldq, _p(k), ldk, _p(v), ldv, _p(q_offsets), _p(kv_starts), _p(kv_lens), M, rows, seqs, max_q_len,
                                      max_kv_len, wq // head_dim, wk // head_dim, head_dim, head_dim ** -0.5 if scale is None else scale,
                                      int(causal), _p(out), ldo, _p(ws), ws_bytes, _stream_handle(stream))
     _check("is_attention", st)
-    _release_workspace(ws, workspace, stream)
     return out
 
 
@@ -1235,7 +1219,7 @@ def is_lora_add(x, a, b, row_adapter, base, scales=None, ranks=None, out=None, w
     if a.get_device() != device or b.get_device() != device:
         raise ValueError(f"a, b: expected tensors on device {device}")
     if out is None:
-        out = _torch().empty((M, N), dtype=_half_dtype, device=x.device)
+        out = _empty((M, N), _half_dtype, x.device, stream)
     ldx, ldo = _rows(x, M, K, device, "x"), _rows(out, M, N, device, "out")
     ldb = _rows(base, M, N, device, "base") if base is not None else 0
     _vector(row_adapter, _int32_dtype, M, device, "row_adapter")
@@ -1243,9 +1227,8 @@ def is_lora_add(x, a, b, row_adapter, base, scales=None, ranks=None, out=None, w
         _vector(scales, _float_dtype, E, device, "scales")
     if ranks is not None:
         _vector(ranks, _int32_dtype, E, device, "ranks")
-    ws, ws_bytes = _workspace(is_lora_workspace_bytes, (M, N, K, R, E), x.device, workspace)
+    ws, ws_bytes = _workspace(is_lora_workspace_bytes, (M, N, K, R, E), x.device, workspace, stream)
     st = load_library().is_lora_add(_p(x), ldx, _p(a), _p(b), _p(row_adapter), _p(scales), _p(ranks), M, N, K, R, E, _p(base), ldb, _p(out),
                                     ldo, _p(ws), ws_bytes, _stream_handle(stream))
     _check("is_lora_add", st)
-    _release_workspace(ws, workspace, stream)
     return out

@@ -52,3 +52,23 @@ def test_prepacked_gemm_with_a_workspace_of_its_own():
     torch.cuda.synchronize()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     del keep
+
+
+def test_new_outputs_leave_alone_what_the_current_stream_still_reads():
+    # a tensor given up on the current stream whose last reader is still queued there: the call's new output must not lie in it
+    g = torch.Generator().manual_seed(7)
+    q = torch.randn((2048, 4096), generator=g).half().to(DEV)
+    pos, freq = torch.arange(2048, dtype=torch.int32, device=DEV), torch.ones(64, device=DEV)
+    k = torch.empty((2048, 0), dtype=torch.float16, device=DEV)
+    want, _ = P.is_qk_norm_rope(q, k, pos, freq, 128)
+    side = torch.cuda.Stream()
+    last = torch.full((2048, 4096), 3.0, dtype=torch.float16, device=DEV)
+    read = torch.zeros_like(last)
+    torch.cuda.synchronize()
+    keep = busy()
+    read.copy_(last)
+    del last
+    got, _ = P.is_qk_norm_rope(q, k, pos, freq, 128, stream=side)
+    torch.cuda.synchronize()
+    assert (read == 3).all() and torch.equal(got, want)
+    del keep

@@ -17,7 +17,7 @@ class Torch:
     """torch with fills that note the stream they are queued on."""
 
     def __init__(self, log):
-        self.log, self.queue = log, [Stream(0)]
+        self.log, self.memory, self.queue = log, [], [Stream(0)]
         self.cuda = self
 
     def __getattr__(self, name):
@@ -34,7 +34,11 @@ class Torch:
 
     def zeros(self, shape, dtype, device):
         self.log.append(("fill", self.queue[-1].cuda_stream))
-        return Tensor(torch.zeros(shape, dtype=dtype))
+        return self.empty(shape, dtype, device).zero_()
+
+    def empty(self, shape, dtype, device):
+        self.memory.append(self.queue[-1].cuda_stream)
+        return Tensor(torch.empty(shape, dtype=dtype))
 
 
 class Tensor(torch.Tensor):
@@ -68,6 +72,7 @@ def log(monkeypatch):
     monkeypatch.setattr(binding, "_require", lambda *a: None)
     for name, dtype in (("_half_dtype", torch.float16), ("_int32_dtype", torch.int32), ("_int64_dtype", torch.int64), ("_float_dtype", torch.float32)):
         monkeypatch.setattr(binding, name, dtype, raising=False)
+    Torch.last = fake
     return got
 
 
@@ -103,3 +108,23 @@ def test_prepacked_calls_zero_a_new_workspace_on_their_stream(log, call, stream)
     call(stream)
     on = 0 if stream is None else 7
     assert log == [("fill", on), ("kernels", on)]
+
+
+half = lambda *s: torch.zeros(s, dtype=torch.float16)  # noqa: E731
+whole = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+
+
+@pytest.mark.parametrize("stream", [None, Stream(7)], ids=["current", "another"])
+@pytest.mark.parametrize("call,count", [
+    (lambda s: binding.is_attention(half(3, 128), half(3, 128), half(3, 128), whole(2), 64, 3, 3, stream=s), 2),
+    (lambda s: binding.is_qk_norm_rope(half(3, 128), half(3, 64), whole(3), torch.zeros(32), 64, v=half(3, 64), stream=s), 3),
+    (lambda s: binding.is_lora_add(half(3, 64), half(2, 8, 64), half(2, 5, 8), whole(3), half(3, 5), stream=s), 2),
+    (lambda s: binding.is_quantize_act_int8_token(X, stream=s), 2),
+    (lambda s: binding.is_quantize_weights_int4_group(X, 128, 10, stream=s), 5),
+    (lambda s: binding.is_linear_w4a8_intscale(X, W.view(1, 8).expand(16, 8), whole(16, 1), None, 128, 10, want_acc=True, stream=s), 3),
+    (lambda s: binding.is_prepack_w4(torch.zeros((16, 64), dtype=torch.uint8), whole(16, 1), 128, stream=s), 2)],
+    ids=["attention", "rotation", "adapters", "quantiser", "weights", "linear", "prepack"])
+def test_new_tensors_are_from_the_calls_stream(log, call, count, stream):
+    # (the current stream's memory may still be in use by work queued there)
+    call(stream)
+    assert Torch.last.memory == [0 if stream is None else 7] * count
