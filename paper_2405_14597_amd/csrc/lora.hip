@@ -383,8 +383,13 @@ __global__ __launch_bounds__(kLoraWaves* kWave) __attribute__((amdgpu_waves_per_
     }
 }
 
-// The form by rows reads an adapter once for every row of it (from L2, mostly), whatever the rows' mix; 2^26 products are 134 MB of such
-// reads on the wider side.
+// The form by rows reads an adapter once for every row of it (from L2, mostly), whatever the rows' mix; a tile walks every adapter in it.
+// Which rows have which adapter is known on the device alone, so that the limit lies between what either mix would want.  On 4096 x 4096
+// the 2^26 products are 1024 rows at rank 16, 256 at rank 64; us by rows / by tiles:
+//              rows in runs of four adapters                an adapter of 32 a row
+//   rank 16    512: 15 / 12   1024: 24 / 19   2048: 41 / 20   512: 18 / 47   1024: 27 / 63   2048: 44 / 115
+//   rank 64    128: 17 / 18    256: 27 / 19    512: 47 / 28   128: 24 / 79    256: 36 / 78    512: 56 / 92
+// and on 28672 x 8192 at rank 64 (36 rows) 16: 19 / 27, 64: 38 / 31 in runs, 19 / 57, 56 / 108 mixed.
 bool by_rows(int M, int N, int K, int R) { return (long long)M * R * std::max(K, N) <= 1LL << 26; }
 
 int lora_slabs(int M, int K) {
