@@ -72,3 +72,13 @@ def test_new_outputs_leave_alone_what_the_current_stream_still_reads():
     torch.cuda.synchronize()
     assert (read == 3).all() and torch.equal(got, want)
     del keep
+
+
+def test_no_rows_on_another_stream():
+    side = torch.cuda.Stream()
+    half = lambda *s: torch.zeros(s, dtype=torch.float16, device=DEV)  # noqa: E731
+    whole = lambda n: torch.zeros(n, dtype=torch.int32, device=DEV)  # noqa: E731
+    assert P.is_lora_add(half(0, 64), half(2, 8, 64), half(2, 40, 8), whole(0), half(0, 40), stream=side).shape == (0, 40)
+    assert P.is_attention(half(0, 128), half(0, 64), half(0, 64), whole(1), 64, 0, 0, stream=side).shape == (0, 128)
+    assert P.is_qk_norm_rope(half(0, 128), half(0, 64), whole(0), torch.zeros(32, device=DEV), 64, stream=side)[0].shape == (0, 128)
+    torch.cuda.synchronize()
