@@ -1047,8 +1047,8 @@ static int check_attention(int M, int num_seqs, int max_q_len, int max_kv_len, i
 size_t is_attention_workspace_bytes(int M, int num_seqs, int max_q_len, int max_kv_len, int heads_q, int heads_kv, int head_dim) {
     if (check_attention(M, num_seqs, max_q_len, max_kv_len, heads_q, heads_kv, head_dim) != IS_OK || M == 0 || num_seqs == 0) return 0;
     const int group = heads_q / heads_kv;
-    const size_t with = attention_workspace_bytes(attention_plan(M, num_seqs, max_q_len, max_kv_len, heads_kv, group, true), M, heads_kv, group, head_dim);
-    const size_t without = attention_workspace_bytes(attention_plan(M, num_seqs, max_q_len, max_kv_len, heads_kv, group, false), M, heads_kv, group, head_dim);
+    const size_t with = attention_workspace_bytes(attention_plan(M, num_seqs, max_q_len, max_kv_len, heads_kv, group, head_dim, true), M, heads_kv, group, head_dim);
+    const size_t without = attention_workspace_bytes(attention_plan(M, num_seqs, max_q_len, max_kv_len, heads_kv, group, head_dim, false), M, heads_kv, group, head_dim);
     return std::max(with, without);  // (whether the call brings kv_lens is not known here)
 }
 
@@ -1068,7 +1068,7 @@ int is_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const v
     if (q_offsets == nullptr || (reinterpret_cast<uintptr_t>(q_offsets) & 3u) || (reinterpret_cast<uintptr_t>(kv_starts) & 7u) ||
         (reinterpret_cast<uintptr_t>(kv_lens) & 3u))
         return IS_ERR_INVALID_ARG;
-    const AttnPlan p = attention_plan(M, num_seqs, max_q_len, max_kv_len, heads_kv, heads_q / heads_kv, kv_lens != nullptr);
+    const AttnPlan p = attention_plan(M, num_seqs, max_q_len, max_kv_len, heads_kv, heads_q / heads_kv, head_dim, kv_lens != nullptr);
     const size_t need = attention_workspace_bytes(p, M, heads_kv, heads_q / heads_kv, head_dim);
     if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return IS_ERR_WORKSPACE;
     AttnArgs a;

@@ -16,6 +16,8 @@
 // instructions 40 %, LDS 19 %, no bank conflicts, 2.0 GHz); few rows (single tokens), bound by memory (64 requests, 1.07 GB: 171 us, 6.2 TB/s;
 // a plain streaming read 6.4).  Not kept for row tiles: the next tile's scores under this tile's probabilities (24 to 84 registers spilled at
 // heads of 128, 1450 us and more; no gain at heads of 64), wave priorities (no change).
+#include <math.h>
+
 #include <algorithm>
 
 #include "block_common.h"
@@ -932,20 +934,33 @@ hipError_t launch_all(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) 
     return hipGetLastError();
 }
 
-// Keys to a workgroup: all of them, or so many that the chip gets `want` workgroups, a multiple of `step` and no fewer than `least`.
-void cut_keys(int max_kv, long long workgroups, int want, int step, int least, int* chunk, int* chunks) {
-    const long long pieces = want / (workgroups < 1 ? 1 : workgroups);
-    const long long whole = ceil_div(max_kv < 1 ? 1 : max_kv, step) * step;
-    long long keys = pieces > 1 ? ceil_div(ceil_div(max_kv, pieces), step) * step : whole;
-    if (keys < least) keys = least;
-    if (keys > whole) keys = whole;
-    *chunk = (int)keys;
-    *chunks = (int)ceil_div(whole, keys);
+// Pieces of the keys for the row tiles, by a fitted time: a unit takes 1.1 us for a tile of keys and one workgroup's rows, 0.9 of it
+// when it has several workgroups (which then take turns, an uneven last turn half filled); two more tiles' time for a workgroup's
+// beginning and end; pieces cost 7 us for a launch and the writing and reading of their partial rows.  Fitted to all numbers of pieces of
+// 129 calls (70 to 4096 rows of 8 to 64 heads over as many keys and up to 60000): 3 % behind the best of each on average, 25 % at most; three
+// workgroups a unit instead, whatever the rows: 17 %, 2.6 times at most.  900 rows over 900 keys, 32 + 8 heads of 128: 24.5 us whole, 42 in
+// two pieces; 300 over 16000: 289 whole, 101 in six, 139 in 32; 128 over 60000: 1085 whole, 147 in sixteen.
+int key_pieces(int M, int max_q, int max_kv, int heads_kv, int group, int head_dim) {
+    const double workgroups = (double)(((long long)M * group / (kTileWaves * kRowsPerWave) + 1) * heads_kv), units = cu_count();
+    const double seen = 1.0 - 0.5 * std::min(max_q, max_kv) / std::max(max_kv, 1);  // (of whole prompts a row sees half)
+    const long long tiles = ceil_div(std::max(max_kv, 1), kKeys), most = std::min(tiles, (long long)(3.0 * units / workgroups) + 1);
+    const double join = (double)M * heads_kv * group * (4 * head_dim + 8) / 4e6;
+    long long best = 1;
+    double least = 0.0;
+    for (long long pieces = 1; pieces <= most; pieces += 1 + pieces / 16) {
+        const long long each = ceil_div(tiles, pieces), n = ceil_div(tiles, each);
+        const double turns = workgroups * n / units;
+        double us = 1.1 * (each + 2);
+        if (turns > 1.0) us = std::max(us, 1.1 * 0.9 * 0.5 * (turns + ceil(turns)) * (each * seen + 2));
+        if (n > 1) us += 7.0 + n * join;
+        if (pieces == 1 || us < least) best = n, least = us;
+    }
+    return (int)best;
 }
 
 }  // namespace
 
-AttnPlan attention_plan(int M, int seqs, int max_q, int max_kv, int heads_kv, int group, bool own_lens) {
+AttnPlan attention_plan(int M, int seqs, int max_q, int max_kv, int heads_kv, int group, int head_dim, bool own_lens) {
     AttnPlan p;
     max_q = std::min(max_q, M);
     const long long most = (long long)max_q * group;
@@ -963,8 +978,11 @@ AttnPlan attention_plan(int M, int seqs, int max_q, int max_kv, int heads_kv, in
         p.slots = (int)std::min(ceil_div(cu_count(), heads_kv), ceil_div(seqs * most, kLeast));
         p.few_cut = p.slots > 1 && (seqs > 1 || most > kLeast);
     }
-    // (three workgroups a unit wanted: a chunk of 300 rows over 4300 keys beside 24 requests 103 us, 106 with two, 126 with one)
-    if (p.tiles) cut_keys(max_kv, ((long long)M * group / (kTileWaves * kRowsPerWave) + 1) * heads_kv, 3 * cu_count(), kKeys, 256, &p.tile_chunk, &p.tile_chunks);
+    if (p.tiles) {
+        const long long tiles = ceil_div(std::max(max_kv, 1), kKeys), each = ceil_div(tiles, key_pieces(M, max_q, max_kv, heads_kv, group, head_dim));
+        p.tile_chunk = (int)(each * kKeys);
+        p.tile_chunks = (int)ceil_div(tiles, each);
+    }
     return p;
 }
 

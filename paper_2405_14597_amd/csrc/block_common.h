@@ -49,7 +49,7 @@ struct AttnPlan {
     int slots = 0, least_tiles = 0;
     bool few_cut = false;            // a sequence may lie in several workgroups' runs
 };
-AttnPlan attention_plan(int M, int seqs, int max_q, int max_kv, int heads_kv, int group, bool own_lens);
+AttnPlan attention_plan(int M, int seqs, int max_q, int max_kv, int heads_kv, int group, int head_dim, bool own_lens);
 size_t attention_workspace_bytes(const AttnPlan& p, int M, int heads_kv, int group, int head_dim);
 hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, int head_dim, void* workspace, hipStream_t stream);
 
