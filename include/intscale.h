@@ -465,7 +465,8 @@ int is_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const v
  *   rows whose adapter lies outside [0, num_adapters) (-1: none) get base[m,n].
  * Sums in single precision; on many rows the sum over k goes into the product with b to 2^-22 of itself (one below 2^-14 of its
  * row's largest: to 2^-35 of that, and to 2^-11 of itself at worst).
- *   x    fp16 [M] rows of K elements, ldx apart;  a  fp16 [num_adapters, R, K];  b  fp16 [num_adapters, N, R]
+ *   x    fp16 [M] rows of K elements, ldx apart: the projection's input, the rows that is_linear_w4a8_* takes (the calls that fold the
+ *        quantiser into a norm or a product write codes alone, no such rows);  a  fp16 [num_adapters, R, K];  b  fp16 [num_adapters, N, R]
  *   row_adapter  int32 [M];  scales  float [num_adapters] or NULL (1);  ranks  int32 [num_adapters] or NULL (R): what lies past an
  *                adapter's rank (rows of a, columns of b) does not count
  *   base, out    fp16 [M] rows of N elements, ldb and ldo apart.  base is the projection's output (NULL: zeros); out may be base

@@ -11,11 +11,13 @@
 // Query rows and the query heads of a key head are one axis ("packed rows": row * group + head), so that a tile of 32 packed
 // rows a wave is full for single tokens of grouped heads too and the keys are read once for the whole group.
 //
-// Two kernels: row tiles (prompts and chunks of them), bound by the matrix instructions, the exponentials beside them and what of both does
-// not overlap (8192 rows, 64 heads of 128: 1076 to 1135 us from box to box, 0.97 to 1.02 PFLOP/s; counters: matrix pipe busy 38 % of the time, vector
-// instructions 40 %, LDS 19 %, no bank conflicts, 2.0 GHz); few rows (single tokens), bound by memory (64 requests, 1.07 GB: 171 us, 6.2 TB/s;
-// a plain streaming read 6.4).  Not kept for row tiles: the next tile's scores under this tile's probabilities (24 to 84 registers spilled at
-// heads of 128, 1450 us and more; no gain at heads of 64), wave priorities (no change).
+// Two kernels: row tiles (prompts and chunks of them), bound by the matrix instructions, the exponentials beside them and the clock that
+// both leave (8192 rows, 64 heads of 128: 1090 to 1155 us from box to box, 0.95 to 1.01 PFLOP/s; counters of that call alone: matrix pipe
+// busy 54 % of the cycles, vector instructions 50 %, LDS 27 %, no bank conflicts, the clock at 1.6 GHz on that box; of heads of 64, both
+// ways, 27 %, 51 %, 14 %: vector instructions, twice the exponentials a product); few rows (single tokens), bound by memory (64 requests,
+// 1.07 GB: 171 us, 6.2 TB/s; a plain streaming read 6.4; drafts of 5 tokens of 32 requests over 4000 keys 90 us at a group of 4, 5.8 TB/s,
+// 115 at a group of 8, whose instance of 64 rows spills 90 registers).  Not kept for row tiles: the next tile's scores under this tile's
+// probabilities (24 to 84 registers spilled at heads of 128, 1450 us and more; no gain at heads of 64), wave priorities (no change).
 #include <math.h>
 
 #include <algorithm>

@@ -3,11 +3,11 @@
 // Two kernels a call: the inner products t = x A_e^T [M, R] in single precision to the workspace, then the outer product added to
 // the base.  Two forms of them:
 //   by rows   every row by itself with its own adapter, on the vector units: a decode step's rows have an adapter each, and
-//             what such a step computes is little; bound by latency (64 rows of 32 adapters, rank 16, 4096 x 4096: 4.9 + 3.3 us where the
-//             tiles take 9 + 27; one row 2.8 + 2.3 us);
+//             what such a step computes is little; bound by latency (64 rows of 32 adapters, rank 16, 4096 x 4096: 3.9 + 2.9 us, 7.2 in
+//             all where the tiles take 40; one row 3.0 + 2.3 us);
 //   by tiles  32 or 64 rows at a time on the matrix units, for prompts, whose rows share an adapter in long runs: bound by the reading
 //             of x and base and the writing of out, of which too little is on its way at a time (4096 rows of nine requests, rank 64,
-//             4096 x 6144: 28 + 46 us, 138 MB at 1.9 TB/s).  A tile walks the adapters that occur in it and keeps each row's own
+//             4096 x 6144: 28 + 40 us, 72 in all, 138 MB at 1.9 TB/s).  A tile walks the adapters that occur in it and keeps each row's own
 //             result (selected, not masked by a factor, so that nothing of one adapter, an infinity for one, reaches another
 //             request's rows).
 #include <algorithm>
@@ -416,8 +416,8 @@ hipError_t launch_lora_add(const LoraArgs& args, void* workspace, hipStream_t st
     const int wide = a.N % 8 == 0 && a.ldo % 8 == 0 && (a.base == nullptr || a.ldb % 8 == 0);
     const dim3 inner((a.M + 16 * kInnerBlocks - 1) / (16 * kInnerBlocks), a.slabs);
     // Four workgroups a unit, each over as many columns as that leaves: every one of them adds up the slabs of t, and with more the
-    // sums take longer, with fewer too little of base is on its way (4096 x 6144, rank 64, three adapters in the worst tile: 46 us; with
-    // 2 and 6 a unit 61 and 54).
+    // sums take longer, with fewer too little of base is on its way (4096 x 6144, rank 64, three adapters in the worst tile: 72 us with the
+    // inner products; with 2 and 6 a unit 83 and 77).
     const int row_tiles = (a.M + kOuterRows - 1) / kOuterRows, col_tiles = (a.N + kOuterCols - 1) / kOuterCols;
     const int steps = std::max(1, col_tiles * row_tiles / (4 * cu_count()));
     const dim3 outer((col_tiles + steps - 1) / steps, row_tiles);
