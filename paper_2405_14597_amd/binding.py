@@ -391,16 +391,18 @@ def _on_stream(make, shape, dtype, device, stream):
 
 def _empty(shape, dtype, device, stream):
     """A call's new output."""
+    if stream is None:
+        return _torch().empty(shape, dtype=dtype, device=device)
     t = _on_stream(_torch().empty, shape, dtype, device, stream)
-    if stream is not None:
-        t.record_stream(_torch().cuda.current_stream())  # (the caller's, who reads it there once it has waited)
+    t.record_stream(_torch().cuda.current_stream())  # (the caller's, who reads it there once it has waited)
     return t
 
 
 def _zeros(shape, dtype, device, stream):
+    if stream is None:
+        return _torch().zeros(shape, dtype=dtype, device=device)
     t = _on_stream(_torch().zeros, shape, dtype, device, stream)
-    if stream is not None:
-        t.record_stream(_torch().cuda.current_stream())
+    t.record_stream(_torch().cuda.current_stream())
     return t
 
 
